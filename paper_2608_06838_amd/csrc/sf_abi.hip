@@ -23,6 +23,7 @@
 #include <utility>
 #include <vector>
 
+#include "sf_host.hpp"
 #include "sf_launch.hpp"
 #include "stateflow.h"
 
@@ -35,21 +36,7 @@ static __device__ __align__(256) unsigned char scratch[SF_NOALLOC_SCRATCH_BYTES]
 
 namespace {
 
-thread_local std::string g_err;
-
-sf_status fail(sf_status s, const char *fmt, ...) {
-    char buf[512];
-    va_list ap;
-    va_start(ap, fmt);
-    vsnprintf(buf, sizeof buf, fmt, ap);
-    va_end(ap);
-    g_err = buf;
-    return s;
-}
-
-sf_status hip_fail(hipError_t e, const char *what) {
-    return fail(SF_E_HIP, "%s: %s", what, hipGetErrorString(e));
-}
+using namespace sf::host;
 
 // Device address of `scratch` on the current device, resolved once per device
 // with that device current.
@@ -79,25 +66,6 @@ struct Shape {
     size_t esz;
     int64_t sx_b, sx_l, sx_h, sg_b, sg_l, sg_h;
 };
-
-struct Dim {
-    int64_t size, stride;
-};
-
-// Strided tensor with a contiguous innermost dim of `inner` elements: the index
-// map is injective iff, sorted by stride, each stride covers the previous extent.
-bool non_overlapping(std::vector<Dim> dims, int64_t inner) {
-    std::vector<Dim> d;
-    for (auto &x : dims)
-        if (x.size > 1) d.push_back(x);
-    std::sort(d.begin(), d.end(), [](const Dim &a, const Dim &b) { return a.stride < b.stride; });
-    int64_t extent = inner;
-    for (auto &x : d) {
-        if (x.stride < extent) return false;
-        extent = x.stride * x.size;
-    }
-    return true;
-}
 
 sf_status resolve(const sf_shape *sh, Shape &r) {
     if (!sh) return fail(SF_E_NULL, "shape is NULL");
@@ -157,17 +125,6 @@ sf_status resolve(const sf_shape *sh, Shape &r) {
     return SF_OK;
 }
 
-// byte extent of a tensor, as integer addresses ([lo, hi); lo = 0 for an
-// absent tensor): no pointer arithmetic on absent (NULL) pointers and no
-// ordering of pointers into different objects
-struct Range {
-    uintptr_t lo, hi;
-    const char *name;
-};
-Range span(const void *p, int64_t bytes, const char *name) {
-    const uintptr_t b = (uintptr_t)p;
-    return {b, b && bytes > 0 ? b + (uintptr_t)bytes : b, name};
-}
 Range xrange(const Shape &r, const void *p, int64_t L, const char *name) {
     const int64_t last = (r.B - 1) * r.sx_b + (L - 1) * r.sx_l + (r.H - 1) * r.sx_h + r.D;
     return span(p, L > 0 ? last * (int64_t)r.esz : 0, name);
@@ -180,52 +137,7 @@ Range grange(const Shape &r, const float *p, int64_t L, const char *name) {
 Range srange(const Shape &r, const float *p, int64_t nstates, const char *name) {
     return span(p, nstates * r.B * r.H * (int64_t)r.D * r.D * 4, name);
 }
-Range wsrange(const void *ws, size_t bytes) { return span(ws, (int64_t)bytes, "ws"); }
-bool overlap(const Range &a, const Range &b) {
-    return a.lo && b.lo && a.lo < a.hi && b.lo < b.hi && a.lo < b.hi && b.lo < a.hi;
-}
-sf_status check_alias(const std::vector<Range> &ins, const std::vector<Range> &outs) {
-    for (size_t i = 0; i < outs.size(); ++i) {
-        for (auto &in : ins)
-            if (overlap(outs[i], in)) return fail(SF_E_ALIAS, "output %s overlaps input %s", outs[i].name, in.name);
-        for (size_t j = i + 1; j < outs.size(); ++j)
-            if (overlap(outs[i], outs[j]))
-                return fail(SF_E_ALIAS, "output %s overlaps output %s", outs[i].name, outs[j].name);
-    }
-    return SF_OK;
-}
-sf_status check_align(std::initializer_list<std::pair<const void *, const char *>> ps) {
-    for (auto &p : ps)
-        if (p.first && ((uintptr_t)p.first % 16))
-            return fail(SF_E_ALIGN, "%s is not 16-byte aligned", p.second);
-    return SF_OK;
-}
-
 // --------------------------------------------------------- plan / workspace
-constexpr size_t ALIGN = 256;
-size_t al(size_t x) { return (x + ALIGN - 1) / ALIGN * ALIGN; }
-
-// Compute units of the current device (256 on MI355X; also the fallback when no
-// device is visible, e.g. for workspace queries on a host without a GPU).
-int device_cus() {
-    static thread_local int cached_dev = -2, cached_cus = 256;
-    int dev = -1;
-    if (hipGetDevice(&dev) != hipSuccess) {
-        (void)hipGetLastError();
-        return 256;
-    }
-    if (dev != cached_dev) {
-        int n = 0;
-        if (hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || n <= 0) {
-            (void)hipGetLastError();
-            n = 256;
-        }
-        cached_dev = dev;
-        cached_cus = n;
-    }
-    return cached_cus;
-}
-
 // Superchunks of one head run one after another inside a workgroup.  The cost
 // of a forward and a backward over ns superchunks of at most m chunks for each of
 // bh heads, in chunk steps, fitted to measured steps of five workloads (2 to 128
@@ -424,33 +336,6 @@ sf_status chain_plan(const Shape &r, int32_t n_seg, const int64_t *seg_len, cons
 // kernel kind whose bit is set takes the next pair of the caller's events as
 // the begin and end timestamps of its own dispatch packets.  The library keeps
 // nothing: the pairs, the count and the kinds live in the caller's record.
-sf_status check_timing(const sf_tuning *t) {
-    if (t && (t->overlap < 0 || t->overlap > 2))
-        return fail(SF_E_SHAPE, "tuning.overlap must be 0, 1 or 2 (got %d)", t->overlap);
-    const sf_timing *tm = t ? t->timing : nullptr;
-    if (!tm) return SF_OK;
-    if (tm->capacity < 0 || tm->count < 0 || tm->count > tm->capacity)
-        return fail(SF_E_SHAPE, "timing: need 0 <= count <= capacity (count=%d capacity=%d)", tm->count,
-                    tm->capacity);
-    if (tm->capacity > 0 && (!tm->start || !tm->stop || !tm->kind))
-        return fail(SF_E_NULL, "timing: start, stop and kind arrays are required");
-    return SF_OK;
-}
-sf_timing *timing_of(const sf_tuning *t) { return t ? t->timing : nullptr; }
-
-void take_pair(sf_timing *tm, int kind, hipEvent_t &e0, hipEvent_t &e1) {
-    e0 = e1 = nullptr;
-    if (!tm || kind < 0 || kind >= 32 || !((tm->mask >> kind) & 1u)) return;
-    if (tm->count >= tm->capacity) {
-        ++tm->dropped;
-        return;
-    }
-    e0 = (hipEvent_t)tm->start[tm->count];
-    e1 = (hipEvent_t)tm->stop[tm->count];
-    tm->kind[tm->count] = kind;
-    ++tm->count;
-}
-
 sf_status launch(int kind, const Shape &r, const sf::SegArgs &a, hipStream_t s, sf_timing *tm) {
     hipEvent_t e0, e1;
     take_pair(tm, kind, e0, e1);
@@ -661,12 +546,6 @@ sf_status dep(hipStream_t from, hipStream_t to, hipEvent_t ev) {
     if (e == hipSuccess) e = hipStreamWaitEvent(to, ev, 0);
     return e == hipSuccess ? SF_OK : hip_fail(e, "stream dependency");
 }
-
-#define TRY(x)                          \
-    do {                                \
-        sf_status _rc = (x);            \
-        if (_rc != SF_OK) return _rc;   \
-    } while (0)
 
 sf_status check_segments(const Shape &r, int32_t n_seg, const int64_t *seg_len) {
     if (n_seg < 1) return fail(SF_E_SHAPE, "n_seg must be >= 1");

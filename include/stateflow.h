@@ -132,7 +132,11 @@ typedef enum {
     SF_K_GDN_DSCAN = 13, /* gated delta rule backward: transposed scan */
     SF_K_GDN_DWALK = 14, /* gated delta rule backward: state-gradient walk */
     SF_K_GDN_DCHUNK = 15, /* gated delta rule backward: per-chunk parameter gradients */
-    SF_K_COUNT = 16
+    SF_K_GDN_TOKENS = 16,  /* ragged gated delta rule: sequences taken token by token */
+    SF_K_CONV_RAGGED = 17, /* ragged short convolution */
+    SF_K_QK_FWD = 18,      /* norms and rotation of queries and keys */
+    SF_K_QK_BWD = 19,      /* their gradients (dq, dk, weight partials and their sums) */
+    SF_K_COUNT = 20
 } sf_kernel_id;
 
 /* Tuning knobs; a NULL pointer selects the defaults for every field. */
@@ -451,6 +455,140 @@ sf_status sf_gdn_chain_bwd(const sf_shape *shape, int32_t n_seg, const int64_t *
                            void *dk, void *dv, float *dg, float *dbeta, float *dS_init, void *ws, size_t ws_bytes,
                            const sf_tuning *tuning, sf_stream main, sf_stream aux);
 
+/*
+ * Ragged batches: N sequences of any lengths packed one behind the other along
+ * the token axis, each with a state (a tail) of its own in a pool of slots that
+ * the calls read and update in place.  What a server runs: single tokens, a few
+ * drafted ones, whole prompts, or all of these in one step.
+ *   T        rows of the packed tensors
+ *   max_len  the longest sequence, as far as the host knows: it chooses how the
+ *            work is launched and never changes what is computed beyond rounding
+ *   cu       device int32 [N + 1]: sequence i is rows cu[i] .. cu[i+1] - 1.  Rows
+ *            before cu[0] and from cu[N] on belong to no sequence: they are not
+ *            read, and outputs there are left as they were.  An entry outside
+ *            [0, T] counts as the nearer end, a sequence that ends before it
+ *            begins as empty; no entry makes a call leave its tensors.
+ *   slot     device int32 [N], the slot of each sequence, or NULL (sequence i has
+ *            slot i).  A sequence whose slot lies outside [0, n_slots) (-1: the
+ *            padding of a batch) is skipped, its outputs left as they were.  Two
+ *            sequences with tokens must not name one slot: what it holds
+ *            afterwards, and their outputs, are unspecified.
+ *   fresh    device uint8 [N] or NULL: where it is not 0 the sequence starts from
+ *            a zero state, whatever its slot holds.
+ * A sequence of no tokens leaves its slot as it was.  Slots that no sequence
+ * names are not touched.
+ */
+typedef struct sf_ragged {
+    int32_t N, n_slots;
+    int64_t T, max_len;
+    const int32_t *cu;
+    const int32_t *slot;
+    const uint8_t *fresh;
+} sf_ragged;
+
+/*
+ * Gated delta rule over a ragged batch, per value head h of a sequence (its key
+ * head is h / (Hv / Hk)):
+ *     S <- exp(g_t) S,   u = beta_t (v_t - S^T k_t),   S <- S + k_t u^T,   o_t = S^T q_t
+ * which is the recurrence of sf_gdn_fwd.
+ *   q, k    [T][Hk][Dk], v, o [T][Hv][Dv] in io_dtype, channels contiguous, element
+ *           strides as given (q and k share theirs); Hk divides Hv
+ *   g, beta float32 [T][Hv], natural-log decay and write strength, element strides
+ *           sg_t, sg_h
+ *   state   float32 [n_slots][Hv][Dk][Dv], the last three packed, ss elements from
+ *           slot to slot; read (unless fresh) and replaced by the state after the
+ *           sequence's last token
+ * Supported: Dk in {64, 128}, Dv in {64, 128, 256}, SF_F32 and SF_BF16 (state,
+ * gates and all arithmetic in fp32 or better), any lengths; pointers 16-byte aligned
+ * (g, beta: 4), strides of q, k, v, o multiples of 16 bytes, ss a multiple of 4.
+ * Inputs may be broadcast (stride 0).  No allocation, no synchronisation.
+ */
+typedef struct sf_gdn_ragged_shape {
+    int32_t Hk, Hv, Dk, Dv;
+    int32_t io_dtype; /* sf_dtype */
+    int32_t reserved; /* must be 0 */
+    int64_t sq_t, sq_h, sv_t, sv_h, so_t, so_h, sg_t, sg_h;
+    int64_t ss;
+} sf_gdn_ragged_shape;
+
+size_t sf_gdn_ragged_workspace_bytes(const sf_gdn_ragged_shape *shape, const sf_ragged *batch);
+sf_status sf_gdn_ragged_fwd(const sf_gdn_ragged_shape *shape, const sf_ragged *batch, const void *q, const void *k,
+                            const void *v, const float *g, const float *beta, float *state, void *o, void *ws,
+                            size_t ws_bytes, const sf_tuning *tuning, sf_stream stream);
+
+/*
+ * Short convolution over a ragged batch: sf_conv_fwd for each sequence, its tail
+ * in a pool of slots and updated in place.
+ *   x, y    [T][C] in io_dtype, channels contiguous, element strides sx_t, sy_t
+ *   w       [C][W] float32, packed
+ *   tails   float32 [n_slots][W-1][C], the last two packed, ss elements from slot to
+ *           slot, oldest input first (W = 1: ignored)
+ * Supported: 1 <= W <= 4, C a multiple of 8, x, y, tails 16-byte aligned, strides of
+ * x and y multiples of 16 bytes, ss a multiple of 4.
+ */
+typedef struct sf_conv_ragged_shape {
+    int32_t C, W;
+    int32_t io_dtype; /* sf_dtype of x and y */
+    int32_t act;      /* sf_act */
+    int32_t reserved; /* must be 0 */
+    int64_t sx_t, sy_t, ss;
+} sf_conv_ragged_shape;
+
+sf_status sf_conv_ragged_fwd(const sf_conv_ragged_shape *shape, const sf_ragged *batch, const void *x, const float *w,
+                             float *tails, void *y, const sf_tuning *tuning, sf_stream stream);
+
+/*
+ * Norms of queries and keys for each head with the position rotation in the same
+ * pass (what stands between the short convolution, or a projection, and the
+ * recurrence or a softmax layer).  Per row x of D channels (one token, one head):
+ *     z = w o (r x),   r = 1 / sqrt(c sum_i x_i^2 + eps),   y = s Rot_t z
+ * with c = 1 (SF_NORM_L2) or 1 / D (SF_NORM_RMS), r = 1 without a norm; w weights
+ * (NULL: ones; one vector for all heads of q, one for k);
+ * s = q_scale for queries, 1 for keys.  Rot_t turns the first R channels in pairs
+ * by the angles p_t inv_freq[i], i < R / 2: channels (i, i + R/2), or (2i, 2i + 1)
+ * when interleaved:  (a, b) -> (a cos - b sin, b cos + a sin).
+ *   q, yq   [B][L][Hq][D],  k, yk [B][L][Hk][D] in io_dtype, channels contiguous,
+ *           element strides as given
+ *   wq, wk  float32 [D] or NULL, both or neither
+ *   inv_freq  float64 [R / 2] (R = 0: ignored); angles are formed and reduced in
+ *           64 bits, so far positions keep their precision
+ *   pos     int64 [B][L] with element strides sp_b, sp_l, or NULL: p_t = pos0 + l
+ * The backward takes dyq, dyk (the strides of yq, yk) and writes dq, dk and, with
+ * weights, dwq, dwk (float32 [D], summed over all rows in a fixed order: bitwise
+ * reproducible); the norm's factor is computed again from q and k.
+ * Supported: D a multiple of 16 up to 256, R a multiple of 16 up to D, 16-byte
+ * aligned pointers and strides (inputs may be broadcast), fewer than 2^31 tokens.
+ */
+typedef enum { SF_NORM_NONE = 0, SF_NORM_L2 = 1, SF_NORM_RMS = 2 } sf_norm;
+
+typedef struct sf_strides {
+    int64_t b, l, h;
+} sf_strides;
+
+typedef struct sf_qk_shape {
+    int32_t B, Hq, Hk, D;
+    int64_t L;
+    int32_t io_dtype;    /* sf_dtype */
+    int32_t norm;        /* sf_norm */
+    int32_t R;           /* rotated channels */
+    int32_t interleaved; /* 0 or 1 */
+    float eps, q_scale;
+    int64_t pos0;
+    int64_t sp_b, sp_l;
+    sf_strides q, k;   /* of the inputs */
+    sf_strides yq, yk; /* of the outputs, or of their gradients (backward) */
+    sf_strides dq, dk; /* of the inputs' gradients (backward) */
+} sf_qk_shape;
+
+sf_status sf_qk_norm_fwd(const sf_qk_shape *shape, const void *q, const void *k, const float *wq, const float *wk,
+                         const double *inv_freq, const int64_t *pos, void *yq, void *yk, const sf_tuning *tuning,
+                         sf_stream stream);
+/* Workspace of the backward (0 without weights). */
+size_t sf_qk_norm_bwd_workspace_bytes(const sf_qk_shape *shape, int32_t weights);
+sf_status sf_qk_norm_bwd(const sf_qk_shape *shape, const void *q, const void *k, const float *wq, const float *wk,
+                         const double *inv_freq, const int64_t *pos, const void *dyq, const void *dyk, void *dq,
+                         void *dk, float *dwq, float *dwk, void *ws, size_t ws_bytes, const sf_tuning *tuning,
+                         sf_stream stream);
 
 #ifdef __cplusplus
 }

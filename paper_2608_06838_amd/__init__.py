@@ -20,6 +20,17 @@ The short convolution whose tail is the auxiliary boundary state of a segment:
 
 x, y: [B, L, C] (bf16 or fp32, channels contiguous); w: [C, W] fp32;
 tails: [B, W-1, C] fp32.
+
+Serving: ragged batches of sequences packed along the token axis, each with a state
+(a tail) in a pool of slots that the calls update in place:
+
+    o                        = gdn_ragged_fwd(q, k, v, g, beta, state, cu_seqlens, slots)
+    y                        = conv_ragged_fwd(x, w, tails, cu_seqlens, slots, act="silu")
+
+Norms of queries and keys for each head, with the position rotation in the same pass:
+
+    q', k'                   = qk_norm_fwd(q, k, norm="l2")
+    dq, dk, dwq, dwk         = qk_norm_bwd(q, k, dq', dk', norm="l2")
 """
 import ctypes
 
@@ -32,7 +43,8 @@ from .timing import KernelTimer  # noqa: F401
 
 __all__ = ["segment_fwd", "segment_fwd_noalloc", "segment_bwd", "chain_ckpt_bytes", "chain_fwd", "chain_bwd", "fwd_workspace_bytes",
            "bwd_workspace_bytes", "chain_workspace_bytes", "conv_fwd", "conv_bwd", "conv_bwd_workspace_bytes",
-           "gdn_fwd", "gdn_fwd_workspace_bytes", "gdn_bwd", "gdn_chain_ckpt_bytes", "gdn_chain_fwd", "gdn_chain_bwd", "partition_hybrid", "KernelTimer", "StateflowError", "abi_version"]
+           "gdn_fwd", "gdn_fwd_workspace_bytes", "gdn_bwd", "gdn_chain_ckpt_bytes", "gdn_chain_fwd", "gdn_chain_bwd", "gdn_ragged_fwd", "conv_ragged_fwd", "qk_norm_fwd",
+           "qk_norm_bwd", "qk_norm_bwd_workspace_bytes", "gdn_ragged_workspace_bytes", "partition_hybrid", "KernelTimer", "StateflowError", "abi_version"]
 
 _IO = {torch.bfloat16: _lib.SF_BF16, torch.float32: _lib.SF_F32}
 _aux_streams = {}
@@ -569,3 +581,247 @@ def partition_hybrid(T, N, alpha, w_tok, w_soft, round_to=128):
     _lib.check("sf_partition_hybrid", _lib.lib().sf_partition_hybrid(int(T), int(N), float(alpha), float(w_tok),
                                                                       float(w_soft), int(round_to), out))
     return [int(x) for x in out]
+
+
+def _on_gpu(ref, **ts):
+    """The library works on device memory of one GPU: a host tensor, or one of another
+    GPU, would reach a kernel as a bad address."""
+    for name, t in ts.items():
+        if t is not None and (not t.is_cuda or t.device != ref.device):
+            raise ValueError(f"{name} must be on {ref.device if ref.is_cuda else 'the GPU'}, it is on {t.device}")
+
+
+def _ragged(T, state, cu_seqlens, slots, fresh, max_len):
+    if cu_seqlens.dim() != 1 or cu_seqlens.dtype != torch.int32 or cu_seqlens.numel() < 1 \
+            or not cu_seqlens.is_contiguous():
+        raise ValueError("cu_seqlens must be a contiguous int32 tensor of N + 1 entries")
+    N = cu_seqlens.numel() - 1
+    if slots is not None and (tuple(slots.shape) != (N,) or slots.dtype != torch.int32 or not slots.is_contiguous()):
+        raise ValueError(f"slots must be a contiguous int32 tensor of {N} entries")
+    if fresh is not None and (tuple(fresh.shape) != (N,) or fresh.dtype not in (torch.uint8, torch.bool)
+                              or not fresh.is_contiguous()):
+        raise ValueError(f"fresh must be a contiguous uint8 or bool tensor of {N} entries")
+    b = _lib.SfRagged()
+    b.N, b.n_slots, b.T = N, N if state is None else state.shape[0], T
+    b.max_len = max(T - N + 1, 1) if max_len is None else int(max_len)
+    b.cu, b.slot, b.fresh = (None if t is None else t.data_ptr() for t in (cu_seqlens, slots, fresh))
+    return b
+
+
+def _gdn_ragged_args(q, k, v, g, beta, state, cu_seqlens, slots, fresh, max_len, o):
+    if q.dim() != 3 or v.dim() != 3:
+        raise ValueError("q, k must be [T, Hk, Dk] and v [T, Hv, Dv]")
+    if q.dtype not in _IO:
+        raise TypeError(f"unsupported I/O dtype {q.dtype}")
+    (T, Hk, Dk), (_, Hv, Dv) = q.shape, v.shape
+    if k.shape != q.shape or k.stride() != q.stride() or k.dtype != q.dtype:
+        raise ValueError("q and k must share shape, strides and dtype")
+    if v.shape[0] != T or v.dtype != q.dtype:
+        raise ValueError("v must have the tokens and the dtype of q")
+    if q.stride(2) != 1 or v.stride(2) != 1:
+        raise ValueError("the channel dim must be contiguous")
+    for name, t in (("g", g), ("beta", beta)):
+        if tuple(t.shape) != (T, Hv) or t.dtype != torch.float32 or t.stride() != g.stride():
+            raise ValueError(f"{name} must be float32 [{T}, {Hv}], with the strides of g")
+    if state.dim() != 4 or tuple(state.shape[1:]) != (Hv, Dk, Dv) or state.dtype != torch.float32 \
+            or (state.numel() and not state[0].is_contiguous()):
+        raise ValueError(f"state must be float32 [slots, {Hv}, {Dk}, {Dv}], contiguous within a slot")
+    if o is not None and (tuple(o.shape) != (T, Hv, Dv) or o.dtype != q.dtype or o.stride(2) != 1):
+        raise ValueError("out must match v in shape and dtype, its channels contiguous")
+    _on_gpu(q, q=q, k=k, v=v, g=g, beta=beta, state=state, cu_seqlens=cu_seqlens, slots=slots, fresh=fresh, out=o)
+    sh = _lib.SfGdnRaggedShape()
+    sh.Hk, sh.Hv, sh.Dk, sh.Dv, sh.io_dtype = Hk, Hv, Dk, Dv, _IO[q.dtype]
+    sh.sq_t, sh.sq_h, sh.sv_t, sh.sv_h = q.stride(0), q.stride(1), v.stride(0), v.stride(1)
+    sh.so_t, sh.so_h = (Hv * Dv, Dv) if o is None else o.stride()[:2]
+    sh.sg_t, sh.sg_h, sh.ss = g.stride(0), g.stride(1), state.stride(0)
+    return sh, _ragged(T, state, cu_seqlens, slots, fresh, max_len)
+
+
+def gdn_ragged_workspace_bytes(q, k, v, g, beta, state, cu_seqlens, slots=None, *, max_len=None):
+    """Bytes of the workspace that gdn_ragged_fwd takes as out[1]."""
+    sh, b = _gdn_ragged_args(q, k, v, g, beta, state, cu_seqlens, slots, None, max_len, None)
+    return _lib.lib().sf_gdn_ragged_workspace_bytes(ctypes.byref(sh), ctypes.byref(b))
+
+
+def gdn_ragged_fwd(q, k, v, g, beta, state, cu_seqlens, slots=None, *, fresh=None, max_len=None, stream=None,
+                   out=None, timing=None):
+    """o of the gated delta rule over a ragged batch; `state` is updated in place.
+
+    q, k: [T, Hk, D]; v: [T, Hv, Dv] (bf16 or fp32, Hk divides Hv: value head h reads
+    key head h // (Hv // Hk)); g (natural-log decay), beta: float32 [T, Hv]; state:
+    float32 [slots, Hv, D, Dv].  Sequence i is rows cu_seqlens[i] .. cu_seqlens[i + 1]
+    - 1 (int32, on the device, N + 1 entries), any number of them, none included; its
+    state is state[slots[i]] (int32; None: state[i]; a slot out of range, such as -1,
+    skips the sequence), or zero where fresh[i] is set, and becomes the state after its
+    last token.  Two sequences with tokens must not share a slot.  Rows of no sequence
+    are left as they were in out=(o, workspace), and undefined in an o allocated here.
+    max_len: the longest sequence if the host knows it (None: taken for N - 1 sequences
+    of one token and one with the rest); it steers the launch, not the result."""
+    o, ws = (None, None) if out is None else out
+    sh, b = _gdn_ragged_args(q, k, v, g, beta, state, cu_seqlens, slots, fresh, max_len, o)
+    stream = stream or torch.cuda.current_stream(q.device)
+    L_ = _lib.lib()
+    with torch.cuda.stream(stream):
+        if out is None:
+            o = torch.empty(v.shape, dtype=v.dtype, device=v.device)
+            ws = _ws(L_.sf_gdn_ragged_workspace_bytes(ctypes.byref(sh), ctypes.byref(b)), q.device)
+        rc = L_.sf_gdn_ragged_fwd(ctypes.byref(sh), ctypes.byref(b), _ptr(q), _ptr(k), _ptr(v), _ptr(g), _ptr(beta),
+                                  _ptr(state), _ptr(o), _ptr(ws), 0 if ws is None else ws.numel() * ws.element_size(),
+                                  ctypes.byref(_tuning(timing=timing)), _stream_handle(stream))
+    _lib.check("sf_gdn_ragged_fwd", rc)
+    return o
+
+
+def conv_ragged_fwd(x, w, tails, cu_seqlens, slots=None, *, fresh=None, act="silu", max_len=None, stream=None,
+                    out=None, timing=None):
+    """y of the short convolution over a ragged batch; `tails` is updated in place.
+
+    x: [T, C] (bf16 or fp32); w: [C, W] float32; tails: float32 [slots, W - 1, C], the
+    oldest input first (None for W = 1).  Sequences, slots, fresh and max_len as for
+    gdn_ragged_fwd.  out: y (a tensor like x) instead of a new one."""
+    if x.dim() != 2 or x.stride(1) != 1:
+        raise ValueError("x must be [T, C] with contiguous channels")
+    if x.dtype not in _IO:
+        raise TypeError(f"unsupported I/O dtype {x.dtype}")
+    T, C = x.shape
+    if w.dim() != 2 or w.shape[0] != C or w.dtype != torch.float32 or not w.is_contiguous():
+        raise ValueError(f"w must be a contiguous float32 [{C}, W] tensor")
+    W = w.shape[1]
+    if W == 1:
+        tails = None
+    elif tails is None or tails.dim() != 3 or tuple(tails.shape[1:]) != (W - 1, C) or tails.dtype != torch.float32 \
+            or (tails.numel() and not tails[0].is_contiguous()):
+        raise ValueError(f"tails must be float32 [slots, {W - 1}, {C}], contiguous within a slot")
+    if out is not None and (out.shape != x.shape or out.dtype != x.dtype or out.stride(1) != 1):
+        raise ValueError("out must match x in shape and dtype, its channels contiguous")
+    if act not in _ACT:
+        raise ValueError(f"act must be one of {sorted(_ACT)}, got {act!r}")
+    _on_gpu(x, x=x, w=w, tails=tails, cu_seqlens=cu_seqlens, slots=slots, fresh=fresh, out=out)
+    b = _ragged(T, tails, cu_seqlens, slots, fresh, max_len)
+    if W == 1 and slots is not None:
+        b.n_slots = 2 ** 31 - 1  # no tails: only negative slots are out of range
+    sh = _lib.SfConvRaggedShape()
+    sh.C, sh.W, sh.io_dtype, sh.act = C, W, _IO[x.dtype], _ACT[act]
+    sh.sx_t, sh.sy_t, sh.ss = x.stride(0), C if out is None else out.stride(0), 0 if tails is None else tails.stride(0)
+    stream = stream or torch.cuda.current_stream(x.device)
+    with torch.cuda.stream(stream):
+        y = torch.empty((T, C), dtype=x.dtype, device=x.device) if out is None else out
+        rc = _lib.lib().sf_conv_ragged_fwd(ctypes.byref(sh), ctypes.byref(b), _ptr(x), _ptr(w), _ptr(tails), _ptr(y),
+                                           ctypes.byref(_tuning(timing=timing)), _stream_handle(stream))
+    _lib.check("sf_conv_ragged_fwd", rc)
+    return y
+
+
+_NORM = {"none": _lib.SF_NORM_NONE, "l2": _lib.SF_NORM_L2, "rms": _lib.SF_NORM_RMS}
+
+
+def _qk_args(q, k, norm, q_weight, k_weight, eps, q_scale, inv_freq, pos, pos0, interleaved, ys, ds):
+    """The call's shape; ys: outputs or their gradients, ds: the inputs' gradients
+    (None: packed)."""
+    if q.dim() != 4 or k.dim() != 4 or q.shape[:2] != k.shape[:2] or q.shape[3] != k.shape[3]:
+        raise ValueError("q and k must be [B, L, Hq, D] and [B, L, Hk, D]")
+    if q.dtype not in _IO:
+        raise TypeError(f"unsupported I/O dtype {q.dtype}")
+    if k.dtype != q.dtype:
+        raise ValueError("q and k must share their dtype")
+    if norm not in _NORM:
+        raise ValueError(f"norm must be one of {sorted(_NORM)}, got {norm!r}")
+    B, L, Hq, D = q.shape
+    for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
+        if w is not None and (tuple(w.shape) != (D,) or w.dtype != torch.float32 or not w.is_contiguous()):
+            raise ValueError(f"{name} must be a contiguous float32 [{D}] tensor")
+    R = 0
+    if inv_freq is not None:
+        if inv_freq.dim() != 1 or inv_freq.dtype != torch.float64 or not inv_freq.is_contiguous():
+            raise ValueError("inv_freq must be a contiguous float64 tensor of R / 2 entries")
+        R = 2 * inv_freq.numel()
+    if pos is not None and (tuple(pos.shape) != (B, L) or pos.dtype != torch.int64):
+        raise ValueError(f"pos must be an int64 [{B}, {L}] tensor")
+    if R == 0:
+        pos = None
+    sh = _lib.SfQkShape()
+    sh.B, sh.L, sh.Hq, sh.Hk, sh.D = B, L, Hq, k.shape[2], D
+    sh.io_dtype, sh.norm, sh.R, sh.interleaved = _IO[q.dtype], _NORM[norm], R, int(bool(interleaved))
+    sh.eps, sh.q_scale, sh.pos0 = float(eps), float(q_scale), int(pos0)
+    if pos is not None:
+        sh.sp_b, sh.sp_l = pos.stride()
+    tensors = dict(q=q, k=k, q_weight=q_weight, k_weight=k_weight, inv_freq=inv_freq, pos=pos)
+    for names, pair in ((("yq", "yk"), ys), (("dq", "dk"), ds)):
+        for name, x, t in zip(names, (q, k), pair):
+            if t is not None and (t.shape != x.shape or t.dtype != x.dtype):
+                raise ValueError(f"{name} must match its input in shape and dtype")
+            tensors[name] = t
+            st = getattr(sh, name)
+            st.b, st.l, st.h = (L * x.shape[2] * D, x.shape[2] * D, D) if t is None else t.stride()[:3]
+    for name, x in tensors.items():
+        if x is not None and x.dim() == 4 and x.stride(3) != 1:
+            raise ValueError(f"{name} must have a contiguous channel dim")
+    for st, x in ((sh.q, q), (sh.k, k)):
+        st.b, st.l, st.h = x.stride()[:3]
+    _on_gpu(q, **tensors)
+    return sh, pos
+
+
+def _packed(x):
+    return torch.empty(x.shape, dtype=x.dtype, device=x.device)
+
+
+def qk_norm_fwd(q, k, *, norm="l2", q_weight=None, k_weight=None, eps=1e-6, q_scale=1.0, inv_freq=None, pos=None,
+                pos0=0, interleaved=False, stream=None, out=None, timing=None):
+    """(q', k'): every head of q [B, L, Hq, D] and k [B, L, Hk, D] normalised over its
+    channels, weighted, its first R channels rotated by the token's position, queries
+    also multiplied by q_scale.
+
+    norm: "l2" (x / sqrt(sum x^2 + eps)), "rms" (x / sqrt(mean x^2 + eps)) or "none";
+    q_weight, k_weight: float32 [D], both or neither.  inv_freq: float64 [R / 2] (None:
+    no rotation), the angle of pair i at position p being p inv_freq[i]; pos: int64
+    [B, L], or None for pos0 + l (pos0: where a segment begins); interleaved: pairs are
+    channels (2i, 2i + 1) instead of (i, i + R / 2).  D: a multiple of 16 up to 256;
+    R: of 16 up to D.  out=(q', k') supplies the outputs, slices of wider rows too."""
+    ys = (None, None) if out is None else out
+    sh, pos = _qk_args(q, k, norm, q_weight, k_weight, eps, q_scale, inv_freq, pos, pos0, interleaved, ys,
+                       (None, None))
+    stream = stream or torch.cuda.current_stream(q.device)
+    with torch.cuda.stream(stream):
+        yq, yk = (_packed(q), _packed(k)) if out is None else out
+        rc = _lib.lib().sf_qk_norm_fwd(ctypes.byref(sh), _ptr(q), _ptr(k), _ptr(q_weight), _ptr(k_weight),
+                                       _ptr(inv_freq), _ptr(pos), _ptr(yq), _ptr(yk),
+                                       ctypes.byref(_tuning(timing=timing)), _stream_handle(stream))
+    _lib.check("sf_qk_norm_fwd", rc)
+    return yq, yk
+
+
+def qk_norm_bwd_workspace_bytes(q, k, dyq, dyk, weights=True):
+    """Bytes of the workspace that qk_norm_bwd takes as out[4] (0 without weights)."""
+    sh, _ = _qk_args(q, k, "l2", None, None, 1e-6, 1.0, None, None, 0, False, (dyq, dyk), (None, None))
+    return _lib.lib().sf_qk_norm_bwd_workspace_bytes(ctypes.byref(sh), int(bool(weights)))
+
+
+def qk_norm_bwd(q, k, dyq, dyk, *, norm="l2", q_weight=None, k_weight=None, eps=1e-6, q_scale=1.0, inv_freq=None,
+                pos=None, pos0=0, interleaved=False, stream=None, out=None, timing=None):
+    """(dq, dk, dwq, dwk) for the loss sum <dyq, q'> + <dyk, k'>; arguments as for
+    qk_norm_fwd.  dwq, dwk (float32 [D], summed over batch, tokens and heads in a fixed
+    order) are None without weights.  out=(dq, dk, dwq, dwk, workspace) supplies the
+    outputs (the last three None without weights)."""
+    dq, dk, dwq, dwk, ws = (None,) * 5 if out is None else out
+    weights = q_weight is not None
+    sh, pos = _qk_args(q, k, norm, q_weight, k_weight, eps, q_scale, inv_freq, pos, pos0, interleaved, (dyq, dyk),
+                       (dq, dk))
+    for name, t in (("dwq", dwq), ("dwk", dwk)):
+        if t is not None and (tuple(t.shape) != (q.shape[3],) or t.dtype != torch.float32 or not t.is_contiguous()):
+            raise ValueError(f"{name} must be a contiguous float32 [{q.shape[3]}] tensor")
+    _on_gpu(q, dwq=dwq, dwk=dwk, workspace=ws)
+    stream = stream or torch.cuda.current_stream(q.device)
+    L_ = _lib.lib()
+    with torch.cuda.stream(stream):
+        if out is None:
+            dq, dk = _packed(q), _packed(k)
+            if weights:
+                dwq, dwk = (torch.empty(q.shape[3], dtype=torch.float32, device=q.device) for _ in range(2))
+                ws = _ws(L_.sf_qk_norm_bwd_workspace_bytes(ctypes.byref(sh), 1), q.device)
+        rc = L_.sf_qk_norm_bwd(ctypes.byref(sh), _ptr(q), _ptr(k), _ptr(q_weight), _ptr(k_weight), _ptr(inv_freq),
+                               _ptr(pos), _ptr(dyq), _ptr(dyk), _ptr(dq), _ptr(dk), _ptr(dwq), _ptr(dwk), _ptr(ws),
+                               0 if ws is None else ws.numel() * ws.element_size(),
+                               ctypes.byref(_tuning(timing=timing)), _stream_handle(stream))
+    _lib.check("sf_qk_norm_bwd", rc)
+    return dq, dk, dwq, dwk

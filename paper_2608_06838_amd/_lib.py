@@ -17,8 +17,10 @@ SF_GATE_SCALAR, SF_GATE_VECTOR = 0, 1
 # sf_kernel_id: the kernel kinds a timing record can select
 KERNELS = {"fwd_prep": 0, "scan": 1, "fwd_out": 2, "bwd_prep": 3, "bwd_dq": 4, "bwd_dkv": 5,
            "conv_fwd": 6, "conv_bwd": 7, "gdn_prep": 8, "gdn_scan": 9, "gdn_out": 10, "gdn_store": 11,
-           "gdn_dprep": 12, "gdn_dscan": 13, "gdn_dwalk": 14, "gdn_dchunk": 15}
+           "gdn_dprep": 12, "gdn_dscan": 13, "gdn_dwalk": 14, "gdn_dchunk": 15, "gdn_tokens": 16, "conv_ragged": 17, "qk_fwd": 18,
+           "qk_bwd": 19}
 SF_ACT_NONE, SF_ACT_SILU = 0, 1
+SF_NORM_NONE, SF_NORM_L2, SF_NORM_RMS = 0, 1, 2
 NOALLOC_SCRATCH_BYTES = 64 << 20  # SF_NOALLOC_SCRATCH_BYTES
 
 # every symbol include/stateflow.h declares
@@ -27,7 +29,8 @@ EXPORTS = ["sf_abi_version", "sf_status_str", "sf_last_error", "sf_fwd_workspace
            "sf_chain_ckpt_bytes", "sf_chain_fwd", "sf_chain_bwd", "sf_conv_bwd_workspace_bytes", "sf_conv_fwd", "sf_conv_bwd",
            "sf_gdn_fwd_workspace_bytes", "sf_gdn_fwd", "sf_gdn_bwd_workspace_bytes", "sf_gdn_bwd",
            "sf_gdn_chain_workspace_bytes", "sf_gdn_chain_ckpt_bytes", "sf_gdn_chain_fwd", "sf_gdn_chain_bwd",
-           "sf_partition_hybrid"]
+           "sf_partition_hybrid", "sf_gdn_ragged_workspace_bytes", "sf_gdn_ragged_fwd", "sf_conv_ragged_fwd",
+           "sf_qk_norm_fwd", "sf_qk_norm_bwd_workspace_bytes", "sf_qk_norm_bwd"]
 
 
 class SfShape(ctypes.Structure):
@@ -53,6 +56,33 @@ class SfTiming(ctypes.Structure):
 class SfTuning(ctypes.Structure):
     _fields_ = [("ts", ctypes.c_int32), ("overlap", ctypes.c_int32),
                 ("reserved", ctypes.c_int32 * 4), ("timing", ctypes.POINTER(SfTiming))]
+
+
+class SfRagged(ctypes.Structure):
+    _fields_ = [("N", ctypes.c_int32), ("n_slots", ctypes.c_int32), ("T", ctypes.c_int64), ("max_len", ctypes.c_int64),
+                ("cu", ctypes.c_void_p), ("slot", ctypes.c_void_p), ("fresh", ctypes.c_void_p)]
+
+
+class SfGdnRaggedShape(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("Hk", "Hv", "Dk", "Dv", "io_dtype", "reserved")] + [
+        (n, ctypes.c_int64) for n in ("sq_t", "sq_h", "sv_t", "sv_h", "so_t", "so_h", "sg_t", "sg_h", "ss")]
+
+
+class SfConvRaggedShape(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("C", "W", "io_dtype", "act", "reserved")] + [
+        (n, ctypes.c_int64) for n in ("sx_t", "sy_t", "ss")]
+
+
+class SfStrides(ctypes.Structure):
+    _fields_ = [("b", ctypes.c_int64), ("l", ctypes.c_int64), ("h", ctypes.c_int64)]
+
+
+class SfQkShape(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("B", "Hq", "Hk", "D")] + [("L", ctypes.c_int64)] + [
+        (n, ctypes.c_int32) for n in ("io_dtype", "norm", "R", "interleaved")] + [
+        ("eps", ctypes.c_float), ("q_scale", ctypes.c_float)] + [
+        (n, ctypes.c_int64) for n in ("pos0", "sp_b", "sp_l")] + [
+        (n, SfStrides) for n in ("q", "k", "yq", "yk", "dq", "dk")]
 
 
 class StateflowError(RuntimeError):
@@ -133,6 +163,21 @@ def lib():
     L.sf_gdn_chain_bwd.argtypes = [sp, i32, i64p] + [vp] * 7 + [sz] + [vp] * 9 + [sz, tp, vp, vp]
     L.sf_partition_hybrid.restype = ctypes.c_int
     L.sf_partition_hybrid.argtypes = [i64, i32, ctypes.c_double, ctypes.c_double, ctypes.c_double, i32, i64p]
+    rp = ctypes.POINTER(SfRagged)
+    gp, xp, kp = (ctypes.POINTER(c) for c in (SfGdnRaggedShape, SfConvRaggedShape, SfQkShape))
+    L.sf_gdn_ragged_workspace_bytes.restype = sz
+    L.sf_gdn_ragged_workspace_bytes.argtypes = [gp, rp]
+    L.sf_gdn_ragged_fwd.restype = ctypes.c_int
+    L.sf_gdn_ragged_fwd.argtypes = [gp, rp] + [vp] * 8 + [sz, tp, vp]
+    L.sf_conv_ragged_fwd.restype = ctypes.c_int
+    L.sf_conv_ragged_fwd.argtypes = [xp, rp] + [vp] * 4 + [tp, vp]
+    L.sf_qk_norm_fwd.restype = ctypes.c_int
+    L.sf_qk_norm_fwd.argtypes = [kp] + [vp] * 8 + [tp, vp]
+    L.sf_qk_norm_bwd_workspace_bytes.restype = sz
+    L.sf_qk_norm_bwd_workspace_bytes.argtypes = [kp, i32]
+    L.sf_qk_norm_bwd.restype = ctypes.c_int
+    # (q, k, wq, wk, inv_freq, pos, dyq, dyk, dq, dk, dwq, dwk, ws, ws_bytes, ...)
+    L.sf_qk_norm_bwd.argtypes = [kp] + [vp] * 13 + [sz, tp, vp]
     _lib = L
     return L
 

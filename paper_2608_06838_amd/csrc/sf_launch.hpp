@@ -133,4 +133,69 @@ enum GdnPhase { GDN_PREP, GDN_SCAN, GDN_OUT, GDN_STORE, GDN_DPREP, GDN_DSCAN, GD
 hipError_t launch_gdn_phase(int phase, const GdnArgs &a, int D, hipStream_t s, hipEvent_t e0, hipEvent_t e1);
 hipError_t launch_conv(bool bwd, const ConvArgs &a, hipStream_t s, hipEvent_t e0, hipEvent_t e1);
 
+
+// Ragged batches (sf_ragged.hip): see sf_ragged in stateflow.h for cu, slot, fresh.
+struct RaggedArgs {
+    const int32_t *cu, *slot;
+    const uint8_t *fresh;
+    int32_t N, n_slots;
+    int64_t T;
+};
+struct GdnRaggedArgs {
+    RaggedArgs r;
+    const void *q, *k, *v;
+    const float *g, *beta;
+    float *state;
+    void *o;
+    int32_t Hk, Hv, Dk, Dv, io, n_cu;
+    int64_t sq_t, sq_h, sv_t, sv_h, so_t, so_h, sg_t, sg_h, ss;
+};
+hipError_t launch_gdn_tokens(const GdnRaggedArgs &a, hipStream_t s, hipEvent_t e0, hipEvent_t e1);
+// waves of that launch: one for each sequence, value head and tile of 4 TOK_CL columns
+constexpr int TOK_CL = 8;
+inline int64_t gdn_token_waves(const GdnRaggedArgs &a) { return (int64_t)a.r.N * a.Hv * (a.Dv / (4 * TOK_CL)); }
+struct ConvRaggedArgs {
+    RaggedArgs r;
+    const void *x;
+    const float *w;
+    float *tails;
+    void *y;
+    int32_t C, W, act, io;
+    int32_t run;     // tokens of one sequence that a thread takes
+    int64_t n_runs;  // upper bound of the runs: T / run + N
+    int64_t sx_t, sy_t, ss;
+};
+hipError_t launch_conv_ragged(const ConvRaggedArgs &a, hipStream_t s, hipEvent_t e0, hipEvent_t e1);
+
+// Norms and rotation of queries and keys (sf_qk.hip).
+struct QkArgs {
+    const void *q, *k, *dyq, *dyk;  // dyq, dyk: backward
+    void *yq, *yk;                  // backward: dq, dk
+    const float *wq, *wk;
+    const double *inv_freq;
+    const int64_t *pos;
+    float *dwq, *dwk, *ws;
+    int32_t B, Hq, Hk, D, io, norm, R, inter;
+    float eps, q_scale;
+    int32_t n_tok;   // B * L
+    int32_t parts;   // waves that share one token's heads
+    int32_t blocks;  // workgroups
+    int64_t L, pos0, sp_b, sp_l;
+    sf_strides sq, sk, syq, syk, sdyq, sdyk;
+};
+constexpr int QK_W = 4, QK_U = 4, QK_UB = 2;  // waves of a workgroup; row groups in flight, forward and backward
+// parts and blocks of a launch, from the shape
+inline void qk_plan(QkArgs &a, bool bwd, int n_cu) {
+    int lpr = 2;  // lanes of a row
+    while (8 * lpr < a.D) lpr *= 2;
+    const int rows = 64 / lpr * (bwd ? QK_UB : QK_U);
+    const int groups = (a.Hq + rows - 1) / rows + (a.Hk + rows - 1) / rows;
+    // a token's row groups are shared between waves until the launch has eight a CU
+    a.parts = 1;
+    while (a.parts < groups && (int64_t)a.n_tok * a.parts < 8 * (int64_t)n_cu) ++a.parts;
+    const int64_t units = (int64_t)a.n_tok * a.parts, blocks = (units + QK_W - 1) / QK_W, most = 8 * (int64_t)n_cu;
+    a.blocks = (int32_t)(blocks < most ? blocks : most);
+}
+hipError_t launch_qk(bool bwd, const QkArgs &a, hipStream_t s, hipEvent_t e0, hipEvent_t e1);
+
 }  // namespace sf

@@ -1,0 +1,281 @@
+// sf_ragged.hip -- gfx950 kernels over ragged batches: sequences of any lengths
+// packed along the token axis, each with a state of its own in a pool of slots,
+// updated in place.
+//
+// Gated delta rule, token by token (S <- e^g S, u = beta (v - S^T k), S <- S + k u^T,
+// o = S^T q).  A single token reads and writes the whole state for 6 flops an
+// element: the roofline is HBM.  State columns (value channels) never mix, so a
+// wave owns CW columns of one head of one sequence and keeps them in registers from
+// the sequence's first token to its last; no LDS, no barrier.  Lane (rg, cl) holds
+// rows rg RPL .. + RPL - 1 of columns 4 cl .. + 3: a row's columns are 16 bytes of
+// 8 consecutive lanes, one 128-byte line, and k and q come as the lane's own run of
+// rows, one or two 16-byte loads that its neighbours share.  With a = e^g and the old
+// state S,
+//     S^T k and S^T q are summed together,   u = beta (v - a S^T k),
+//     o = a S^T q + (k . q) u,               S <- a S + k u^T,
+// so a token costs one reduction over the row groups, of nine sums.
+#include "sf_chunk.hpp"
+
+#include <type_traits>
+
+namespace sf {
+
+namespace {
+
+// A sequence's rows [begin, end) and slot; end <= begin or slot < 0: nothing to do.
+struct Seq {
+    int64_t begin, end;
+    int slot;
+};
+__device__ __forceinline__ int64_t clamp_row(int64_t x, int64_t T) { return x < 0 ? 0 : x > T ? T : x; }
+__device__ __forceinline__ Seq seq_of(const RaggedArgs &r, int i) {
+    Seq s;
+    s.begin = clamp_row(r.cu[i], r.T);
+    s.end = clamp_row(r.cu[i + 1], r.T);
+    s.slot = r.slot ? r.slot[i] : i;
+    if (s.slot >= r.n_slots) s.slot = -1;
+    return s;
+}
+
+// ------------------------------------------------- gated delta rule, token by token
+constexpr int TOK_NT = 256;
+
+// sum over the row groups (lanes that differ in the bits from CL up), in every lane
+template <int CL>
+__device__ __forceinline__ float group_sum(float x) {
+    static_assert(CL == 4 || CL == 8, "column lanes");
+    x += dpp_or0<0x128>(x);                       // row_ror:8
+    if constexpr (CL == 4) x += dpp_or0<0x124>(x);  // row_ror:4
+    return sum_rows(x);
+}
+
+template <typename T, int N> struct Vec { typedef T type __attribute__((ext_vector_type(N))); };
+
+template <typename T, int DK, int CL>
+__global__ void __launch_bounds__(TOK_NT) k_gdn_tokens(GdnRaggedArgs a) {
+    constexpr int CW = 4 * CL, RG = 64 / CL, RPL = DK / RG;
+    typedef typename Vec<T, RPL>::type rows_t;
+    typedef typename Vec<T, 4>::type cols_t;
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int nt = a.Dv / CW;
+    const int64_t unit = (int64_t)blockIdx.x * (TOK_NT / 64) + w;
+    const int tile = (int)(unit % nt);
+    const int64_t ih = unit / nt;
+    const int h = (int)(ih % a.Hv);
+    const int64_t i = ih / a.Hv;
+    if (i >= a.r.N) return;
+    const Seq sq = seq_of(a.r, (int)i);
+    if (sq.end <= sq.begin || sq.slot < 0) return;
+    const int rg = lane / CL, col = tile * CW + 4 * (lane % CL), hk = h / (a.Hv / a.Hk);
+    float *const sp = a.state + sq.slot * a.ss + (int64_t)h * DK * a.Dv + (int64_t)rg * RPL * a.Dv + col;
+    f32x4 S[RPL];
+    const bool fresh = a.r.fresh && a.r.fresh[i];
+#pragma unroll
+    for (int m = 0; m < RPL; ++m) S[m] = fresh ? f32x4{0.f, 0.f, 0.f, 0.f} : *reinterpret_cast<const f32x4 *>(sp + (int64_t)m * a.Dv);
+    const T *kp = (const T *)a.k + hk * a.sq_h + rg * RPL, *qp = (const T *)a.q + hk * a.sq_h + rg * RPL;
+    const T *vp = (const T *)a.v + h * a.sv_h + col;
+    T *op = (T *)a.o + h * a.so_h + col;
+    const float *gp = a.g + h * a.sg_h, *bp = a.beta + h * a.sg_h;
+    rows_t kn = *reinterpret_cast<const rows_t *>(kp + sq.begin * a.sq_t);
+    rows_t qn = *reinterpret_cast<const rows_t *>(qp + sq.begin * a.sq_t);
+    cols_t vn = *reinterpret_cast<const cols_t *>(vp + sq.begin * a.sv_t);
+    float gn = gp[sq.begin * a.sg_t], bn = bp[sq.begin * a.sg_t];
+    for (int64_t t = sq.begin; t < sq.end; ++t) {
+        const rows_t kt = kn, qt = qn;
+        const cols_t vt = vn;
+        const float al = fexp2(gn * LOG2E), be = bn;
+        if (t + 1 < sq.end) {  // the next token's, a step ahead
+            kn = *reinterpret_cast<const rows_t *>(kp + (t + 1) * a.sq_t);
+            qn = *reinterpret_cast<const rows_t *>(qp + (t + 1) * a.sq_t);
+            vn = *reinterpret_cast<const cols_t *>(vp + (t + 1) * a.sv_t);
+            gn = gp[(t + 1) * a.sg_t];
+            bn = bp[(t + 1) * a.sg_t];
+        }
+        f32x4 sk = {0.f, 0.f, 0.f, 0.f}, sv = sk;
+        float kq = 0.f;
+#pragma unroll
+        for (int m = 0; m < RPL; ++m) {
+            const float km = (float)kt[m], qm = (float)qt[m];
+            kq = fmaf(km, qm, kq);
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                sk[c] = fmaf(S[m][c], km, sk[c]);
+                sv[c] = fmaf(S[m][c], qm, sv[c]);
+            }
+        }
+        kq = group_sum<CL>(kq);
+        f32x4 u = {0.f, 0.f, 0.f, 0.f}, o = u;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            u[c] = be * ((float)vt[c] - al * group_sum<CL>(sk[c]));
+            o[c] = fmaf(kq, u[c], al * group_sum<CL>(sv[c]));
+        }
+#pragma unroll
+        for (int m = 0; m < RPL; ++m) {
+            const float km = (float)kt[m];
+#pragma unroll
+            for (int c = 0; c < 4; ++c) S[m][c] = fmaf(km, u[c], al * S[m][c]);
+        }
+        if (rg == 0) {
+            T *p = op + t * a.so_t;
+            if constexpr (sizeof(T) == 2) st4(p, o[0], o[1], o[2], o[3]);
+            else *reinterpret_cast<f32x4 *>(p) = o;
+        }
+    }
+#pragma unroll
+    for (int m = 0; m < RPL; ++m) *reinterpret_cast<f32x4 *>(sp + (int64_t)m * a.Dv) = S[m];
+}
+
+template <typename T>
+hipError_t gdn_tokens_t(const GdnRaggedArgs &a, hipStream_t s, hipEvent_t e0, hipEvent_t e1) {
+    const dim3 grid((unsigned)((gdn_token_waves(a) + TOK_NT / 64 - 1) / (TOK_NT / 64)));
+    if (a.Dk == 128) hipExtLaunchKernelGGL((k_gdn_tokens<T, 128, TOK_CL>), grid, dim3(TOK_NT), 0, s, e0, e1, 0, a);
+    else hipExtLaunchKernelGGL((k_gdn_tokens<T, 64, TOK_CL>), grid, dim3(TOK_NT), 0, s, e0, e1, 0, a);
+    return hipGetLastError();
+}
+
+// ------------------------------------------------------------------ short convolution
+// u_t = sum_j w_j xh_{t-W+1+j}, y_t = act(u_t), each sequence preceded by its slot's
+// tail.  Streaming work like the training form: a thread takes 8 consecutive channels
+// and a run of tokens of one sequence.  The run's sequence is found by counting: run
+// numbers start at cu[i] / run + i, which leaves every sequence room for its own
+// ceil(n / run) runs, so the launch needs neither the lengths on the host nor a table.
+// The sequence's first run alone reads the old tail, and it writes the new one, after
+// that read, from the sequence's last rows, so the pool is updated in place with no
+// order between workgroups.
+constexpr int CR_NT = 256;
+
+// the last sequence i in [0, N) whose first run is <= id; 64 candidates a step
+__device__ __forceinline__ int find_seq(const RaggedArgs &r, int run, int64_t id) {
+    const int lane = threadIdx.x & 63;
+    int lo = 0, n = r.N;
+    while (n > 1) {
+        const int step = (n + 63) / 64, i = lo + lane * step;
+        const bool in = lane * step < n && clamp_row(r.cu[lane * step < n ? i : lo], r.T) / run + i <= id;
+        const int m = __popcll(__ballot(in));
+        const int at = m > 0 ? (m - 1) * step : 0;
+        lo += at;
+        n = n - at < step ? n - at : step;
+    }
+    return __builtin_amdgcn_readfirstlane(lo);
+}
+
+template <bool SILU>
+__device__ __forceinline__ float conv_act(float u) {
+    if constexpr (SILU) return u / (1.f + fexp2(-u * LOG2E));
+    else return u;
+}
+
+template <typename T>
+__device__ __forceinline__ void ld8(const T *p, float (&f)[8]) {
+    const f32x4 lo = ld4f(p), hi = ld4f(p + 4);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        f[e] = lo[e];
+        f[4 + e] = hi[e];
+    }
+}
+
+template <typename T, int W, bool SILU>
+__global__ void __launch_bounds__(CR_NT) k_conv_ragged(ConvRaggedArgs a) {
+    const int nb = (a.C / 8 + (int)blockDim.x - 1) / (int)blockDim.x;  // workgroups of a run
+    const int c0 = 8 * ((int)(blockIdx.x % nb) * (int)blockDim.x + (int)threadIdx.x);
+    const int64_t id = blockIdx.x / nb;
+    const int i = find_seq(a.r, a.run, id);
+    const Seq sq = seq_of(a.r, i);
+    const int64_t t0 = (id - (sq.begin / a.run + i)) * a.run, n = sq.end - sq.begin;
+    if (t0 < 0 || t0 >= n || sq.slot < 0 || c0 >= a.C) return;
+    const int64_t t1 = t0 + a.run < n ? t0 + a.run : n;
+    const T *x = (const T *)a.x + sq.begin * a.sx_t + c0;
+    T *y = (T *)a.y + sq.begin * a.sy_t + c0;
+    float wt[W][8], h[W][8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+#pragma unroll
+        for (int j = 0; j < W; ++j) wt[j][e] = a.w[(int64_t)(c0 + e) * W + j];
+    float *const tail = a.tails + sq.slot * a.ss + c0;
+    if (t0 == 0) {
+        const bool fresh = a.r.fresh && a.r.fresh[i];
+#pragma unroll
+        for (int j = 0; j < W - 1; ++j) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) h[j][e] = 0.f;
+            if (!fresh) ld8<float>(tail + (int64_t)j * a.C, h[j]);
+        }
+        float nt[W][8];  // the new tail: entries W - 1 + n - (W - 1) + j of the old one, then x
+#pragma unroll
+        for (int j = 0; j < W - 1; ++j) {
+            const int64_t s = n - (W - 1) + j;
+            if (s >= 0) {
+                ld8<T>(x + s * a.sx_t, nt[j]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    float v = 0.f;
+#pragma unroll
+                    for (int o = 0; o < W - 1; ++o) v = s + W - 1 == o ? h[o][e] : v;
+                    nt[j][e] = v;
+                }
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < W - 1; ++j) {
+            st4(tail + (int64_t)j * a.C, nt[j][0], nt[j][1], nt[j][2], nt[j][3]);
+            st4(tail + (int64_t)j * a.C + 4, nt[j][4], nt[j][5], nt[j][6], nt[j][7]);
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < W - 1; ++j) ld8<T>(x + (t0 - (W - 1) + j) * a.sx_t, h[j]);
+    }
+    for (int64_t t = t0; t < t1; ++t) {
+        ld8<T>(x + t * a.sx_t, h[W - 1]);
+        float o[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            float u = 0.f;
+#pragma unroll
+            for (int j = 0; j < W; ++j) u = fmaf(wt[j][e], h[j][e], u);
+            o[e] = conv_act<SILU>(u);
+        }
+        T *p = y + t * a.sy_t;
+        if constexpr (sizeof(T) == 2) {
+            bf16x8 v = {};
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = (__bf16)o[e];
+            *reinterpret_cast<bf16x8 *>(p) = v;
+        } else {
+            st4(p, o[0], o[1], o[2], o[3]);
+            st4(p + 4, o[4], o[5], o[6], o[7]);
+        }
+#pragma unroll
+        for (int j = 0; j < W - 1; ++j)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) h[j][e] = h[j + 1][e];
+    }
+}
+
+template <typename T, bool SILU>
+hipError_t conv_ragged_t(const ConvRaggedArgs &a, hipStream_t s, hipEvent_t e0, hipEvent_t e1) {
+    const int ncg = a.C / 8, nt = std::min(CR_NT, (ncg + 63) / 64 * 64);
+    const dim3 grid((unsigned)((ncg + nt - 1) / nt * a.n_runs)), block((unsigned)nt);
+    switch (a.W) {
+    case 1: hipExtLaunchKernelGGL((k_conv_ragged<T, 1, SILU>), grid, block, 0, s, e0, e1, 0, a); break;
+    case 2: hipExtLaunchKernelGGL((k_conv_ragged<T, 2, SILU>), grid, block, 0, s, e0, e1, 0, a); break;
+    case 3: hipExtLaunchKernelGGL((k_conv_ragged<T, 3, SILU>), grid, block, 0, s, e0, e1, 0, a); break;
+    default: hipExtLaunchKernelGGL((k_conv_ragged<T, 4, SILU>), grid, block, 0, s, e0, e1, 0, a); break;
+    }
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_gdn_tokens(const GdnRaggedArgs &a, hipStream_t s, hipEvent_t e0, hipEvent_t e1) {
+    return a.io == SF_BF16 ? gdn_tokens_t<__bf16>(a, s, e0, e1) : gdn_tokens_t<float>(a, s, e0, e1);
+}
+
+hipError_t launch_conv_ragged(const ConvRaggedArgs &a, hipStream_t s, hipEvent_t e0, hipEvent_t e1) {
+    if (a.io == SF_BF16) return a.act ? conv_ragged_t<__bf16, true>(a, s, e0, e1) : conv_ragged_t<__bf16, false>(a, s, e0, e1);
+    return a.act ? conv_ragged_t<float, true>(a, s, e0, e1) : conv_ragged_t<float, false>(a, s, e0, e1);
+}
+
+}  // namespace sf

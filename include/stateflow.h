@@ -136,7 +136,9 @@ typedef enum {
     SF_K_CONV_RAGGED = 17, /* ragged short convolution */
     SF_K_QK_FWD = 18,      /* norms and rotation of queries and keys */
     SF_K_QK_BWD = 19,      /* their gradients (dq, dk, weight partials and their sums) */
-    SF_K_COUNT = 20
+    SF_K_GDN_CHUNK_PREP = 20, /* ragged gated delta rule: triangular systems of the long sequences' chunks */
+    SF_K_GDN_CHUNK_WALK = 21, /* ragged gated delta rule: walk over those chunks */
+    SF_K_COUNT = 22
 } sf_kernel_id;
 
 /* Tuning knobs; a NULL pointer selects the defaults for every field. */
@@ -466,8 +468,9 @@ sf_status sf_gdn_chain_bwd(const sf_shape *shape, int32_t n_seg, const int64_t *
  *   cu       device int32 [N + 1]: sequence i is rows cu[i] .. cu[i+1] - 1.  Rows
  *            before cu[0] and from cu[N] on belong to no sequence: they are not
  *            read, and outputs there are left as they were.  An entry outside
- *            [0, T] counts as the nearer end, a sequence that ends before it
- *            begins as empty; no entry makes a call leave its tensors.
+ *            [0, T] counts as the nearer end.  The entries must not decrease:
+ *            where they do, what the call writes to the rows and slots they name
+ *            is unspecified, but no entry makes it leave its tensors.
  *   slot     device int32 [N], the slot of each sequence, or NULL (sequence i has
  *            slot i).  A sequence whose slot lies outside [0, n_slots) (-1: the
  *            padding of a batch) is skipped, its outputs left as they were.  Two
@@ -502,6 +505,9 @@ typedef struct sf_ragged {
  * gates and all arithmetic in fp32 or better), any lengths; pointers 16-byte aligned
  * (g, beta: 4), strides of q, k, v, o multiples of 16 bytes, ss a multiple of 4.
  * Inputs may be broadcast (stride 0).  No allocation, no synchronisation.
+ * Short sequences, and all with SF_F32, run token by token; with SF_BF16 and a max_len
+ * above 16, longer ones run in chunks of 64 tokens, which takes the workspace (contents
+ * on entry ignored, 16-byte aligned).
  */
 typedef struct sf_gdn_ragged_shape {
     int32_t Hk, Hv, Dk, Dv;

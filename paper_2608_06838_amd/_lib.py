@@ -18,7 +18,7 @@ SF_GATE_SCALAR, SF_GATE_VECTOR = 0, 1
 KERNELS = {"fwd_prep": 0, "scan": 1, "fwd_out": 2, "bwd_prep": 3, "bwd_dq": 4, "bwd_dkv": 5,
            "conv_fwd": 6, "conv_bwd": 7, "gdn_prep": 8, "gdn_scan": 9, "gdn_out": 10, "gdn_store": 11,
            "gdn_dprep": 12, "gdn_dscan": 13, "gdn_dwalk": 14, "gdn_dchunk": 15, "gdn_tokens": 16, "conv_ragged": 17, "qk_fwd": 18,
-           "qk_bwd": 19}
+           "qk_bwd": 19, "gdn_chunk_prep": 20, "gdn_chunk_walk": 21}
 SF_ACT_NONE, SF_ACT_SILU = 0, 1
 SF_NORM_NONE, SF_NORM_L2, SF_NORM_RMS = 0, 1, 2
 NOALLOC_SCRATCH_BYTES = 64 << 20  # SF_NOALLOC_SCRATCH_BYTES

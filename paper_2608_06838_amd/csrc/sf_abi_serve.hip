@@ -106,6 +106,16 @@ sf_status check_gdn(const sf_gdn_ragged_shape *s, const sf_ragged *b) {
     return check_out("o", {{b->T, s->so_t}, {s->Hv, s->so_h}}, s->Dv, e);
 }
 
+// Sequences of more than RAG_LONG tokens are taken in chunks where the operands are
+// bf16 and the host knows of such a sequence; fp32 operands go token by token.
+int gdn_longer(const sf_gdn_ragged_shape &s, const sf_ragged &b) {
+    return s.io_dtype == SF_BF16 && b.max_len > sf::RAG_LONG ? sf::RAG_LONG : 0;
+}
+int64_t gdn_chunks(const sf_ragged &b) { return b.T / 64 + b.N; }
+size_t gdn_ragged_ws_bytes(const sf_gdn_ragged_shape &s, const sf_ragged &b) {
+    return b.N > 0 && b.T > 0 && gdn_longer(s, b) ? (size_t)gdn_chunks(b) * (size_t)s.Hv * sf::RAG_SYS : 0;
+}
+
 // ------------------------------------------------------------- norms and rotation
 sf_status check_qk(const sf_qk_shape *s, bool bwd) {
     if (!s) return fail(SF_E_NULL, "shape is NULL");
@@ -224,6 +234,7 @@ size_t sf_gdn_ragged_workspace_bytes(const sf_gdn_ragged_shape *shape, const sf_
     size_t n = 0;
     (void)guarded([&]() -> sf_status {
         TRY(check_gdn(shape, batch));
+        n = gdn_ragged_ws_bytes(*shape, *batch);
         return SF_OK;
     });
     return n;
@@ -232,18 +243,19 @@ size_t sf_gdn_ragged_workspace_bytes(const sf_gdn_ragged_shape *shape, const sf_
 sf_status sf_gdn_ragged_fwd(const sf_gdn_ragged_shape *shape, const sf_ragged *batch, const void *q, const void *k,
                             const void *v, const float *g, const float *beta, float *state, void *o, void *ws,
                             size_t ws_bytes, const sf_tuning *tuning, sf_stream stream) {
-    (void)ws;
-    (void)ws_bytes;
     return guarded([&]() -> sf_status {
         TRY(check_gdn(shape, batch));
         TRY(check_timing(tuning));
         const sf_gdn_ragged_shape &s = *shape;
         const sf_ragged &b = *batch;
+        const size_t need = gdn_ragged_ws_bytes(s, b);
         if (b.N == 0 || b.T == 0) return SF_OK;  // no sequence has a token
         const int64_t per = (int64_t)s.Hv * s.Dk * s.Dv;
         TRY(check_pool("state", state, b.n_slots, per, s.ss, true));
         if (!q || !k || !v || !g || !beta || !o) return fail(SF_E_NULL, "q, k, v, g, beta and o are required");
-        TRY(check_align({{q, "q"}, {k, "k"}, {v, "v"}, {o, "o"}, {state, "state"}}));
+        if (need > 0 && (!ws || ws_bytes < need))
+            return fail(SF_E_WORKSPACE, "workspace of %zu bytes needed (got %zu)", need, ws ? ws_bytes : (size_t)0);
+        TRY(check_align({{q, "q"}, {k, "k"}, {v, "v"}, {o, "o"}, {state, "state"}, {need ? ws : nullptr, "ws"}}));
         if ((uintptr_t)g % 4 || (uintptr_t)beta % 4) return fail(SF_E_ALIGN, "g and beta must be 4-byte aligned");
         const size_t e = elem_size(s.io_dtype);
         TRY(check_alias({strided(q, {{b.T, s.sq_t}, {s.Hk, s.sq_h}}, s.Dk, e, "q"),
@@ -253,7 +265,7 @@ sf_status sf_gdn_ragged_fwd(const sf_gdn_ragged_shape *shape, const sf_ragged *b
                          strided(beta, {{b.T, s.sg_t}, {s.Hv, s.sg_h}}, 1, 4, "beta"), cu_range(b), slot_range(b),
                          fresh_range(b)},
                         {strided(o, {{b.T, s.so_t}, {s.Hv, s.so_h}}, s.Dv, e, "o"),
-                         pool_range("state", state, b.n_slots, per, s.ss)}));
+                         pool_range("state", state, b.n_slots, per, s.ss), wsrange(need ? ws : nullptr, need)}));
         if (b.n_slots == 0) return SF_OK;  // every slot is out of range
         sf::GdnRaggedArgs a{};
         a.r = ragged_args(b);
@@ -279,8 +291,17 @@ sf_status sf_gdn_ragged_fwd(const sf_gdn_ragged_shape *shape, const sf_ragged *b
         a.sg_t = s.sg_t;
         a.sg_h = s.sg_h;
         a.ss = s.ss;
-        TRY(grid_fits((double)sf::gdn_token_waves(a)));
+        a.longer = gdn_longer(s, b);
+        a.n_chunks = gdn_chunks(b);
+        a.ws = (char *)ws;
+        TRY(grid_fits(std::max((double)sf::gdn_token_waves(a), (double)a.n_chunks * s.Hk)));
         hipEvent_t e0, e1;
+        if (a.longer) {
+            take_pair(timing_of(tuning), SF_K_GDN_CHUNK_PREP, e0, e1);
+            TRY(launched(sf::launch_gdn_chunk_prep(a, (hipStream_t)stream, e0, e1)));
+            take_pair(timing_of(tuning), SF_K_GDN_CHUNK_WALK, e0, e1);
+            TRY(launched(sf::launch_gdn_chunk_walk(a, (hipStream_t)stream, e0, e1)));
+        }
         take_pair(timing_of(tuning), SF_K_GDN_TOKENS, e0, e1);
         return launched(sf::launch_gdn_tokens(a, (hipStream_t)stream, e0, e1));
     });

@@ -149,7 +149,17 @@ struct GdnRaggedArgs {
     void *o;
     int32_t Hk, Hv, Dk, Dv, io, n_cu;
     int64_t sq_t, sq_h, sv_t, sv_h, so_t, so_h, sg_t, sg_h, ss;
+    int32_t longer;    // sequences of more tokens are taken in chunks (0: none are)
+    int64_t n_chunks;  // upper bound of the chunks: T / 64 + N
+    char *ws;          // chunk systems: [n_chunks][Hv] of RAG_SYS bytes
 };
+// A chunk's triangular system, as operand fragments: T = (I + A)^-1 in three bf16
+// planes (exact), P in two, six fragments of 1 KB a plane (sf_ragged_chunk.hip)
+constexpr int RAG_FRAGS = 6, RAG_TP = 3, RAG_PP = 2, RAG_SYS = (RAG_TP + RAG_PP) * RAG_FRAGS * 1024;
+constexpr int RAG_NW = 4;  // waves of a walk workgroup, 16 value columns each
+constexpr int RAG_LONG = 16;
+hipError_t launch_gdn_chunk_prep(const GdnRaggedArgs &a, hipStream_t s, hipEvent_t e0, hipEvent_t e1);
+hipError_t launch_gdn_chunk_walk(const GdnRaggedArgs &a, hipStream_t s, hipEvent_t e0, hipEvent_t e1);
 hipError_t launch_gdn_tokens(const GdnRaggedArgs &a, hipStream_t s, hipEvent_t e0, hipEvent_t e1);
 // waves of that launch: one for each sequence, value head and tile of 4 TOK_CL columns
 constexpr int TOK_CL = 8;

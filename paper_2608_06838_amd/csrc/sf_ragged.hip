@@ -14,28 +14,13 @@
 //     S^T k and S^T q are summed together,   u = beta (v - a S^T k),
 //     o = a S^T q + (k . q) u,               S <- a S + k u^T,
 // so a token costs one reduction over the row groups, of nine sums.
-#include "sf_chunk.hpp"
+#include "sf_ragged.hpp"
 
 #include <type_traits>
 
 namespace sf {
 
 namespace {
-
-// A sequence's rows [begin, end) and slot; end <= begin or slot < 0: nothing to do.
-struct Seq {
-    int64_t begin, end;
-    int slot;
-};
-__device__ __forceinline__ int64_t clamp_row(int64_t x, int64_t T) { return x < 0 ? 0 : x > T ? T : x; }
-__device__ __forceinline__ Seq seq_of(const RaggedArgs &r, int i) {
-    Seq s;
-    s.begin = clamp_row(r.cu[i], r.T);
-    s.end = clamp_row(r.cu[i + 1], r.T);
-    s.slot = r.slot ? r.slot[i] : i;
-    if (s.slot >= r.n_slots) s.slot = -1;
-    return s;
-}
 
 // ------------------------------------------------- gated delta rule, token by token
 constexpr int TOK_NT = 256;
@@ -65,7 +50,7 @@ __global__ void __launch_bounds__(TOK_NT) k_gdn_tokens(GdnRaggedArgs a) {
     const int64_t i = ih / a.Hv;
     if (i >= a.r.N) return;
     const Seq sq = seq_of(a.r, (int)i);
-    if (sq.end <= sq.begin || sq.slot < 0) return;
+    if (sq.end <= sq.begin || sq.slot < 0 || (a.longer && sq.end - sq.begin > a.longer)) return;
     const int rg = lane / CL, col = tile * CW + 4 * (lane % CL), hk = h / (a.Hv / a.Hk);
     float *const sp = a.state + sq.slot * a.ss + (int64_t)h * DK * a.Dv + (int64_t)rg * RPL * a.Dv + col;
     f32x4 S[RPL];
@@ -137,28 +122,10 @@ hipError_t gdn_tokens_t(const GdnRaggedArgs &a, hipStream_t s, hipEvent_t e0, hi
 // ------------------------------------------------------------------ short convolution
 // u_t = sum_j w_j xh_{t-W+1+j}, y_t = act(u_t), each sequence preceded by its slot's
 // tail.  Streaming work like the training form: a thread takes 8 consecutive channels
-// and a run of tokens of one sequence.  The run's sequence is found by counting: run
-// numbers start at cu[i] / run + i, which leaves every sequence room for its own
-// ceil(n / run) runs, so the launch needs neither the lengths on the host nor a table.
-// The sequence's first run alone reads the old tail, and it writes the new one, after
+// and a run of tokens of one sequence (find_seq).  The sequence's first run alone reads the old tail, and it writes the new one, after
 // that read, from the sequence's last rows, so the pool is updated in place with no
 // order between workgroups.
 constexpr int CR_NT = 256;
-
-// the last sequence i in [0, N) whose first run is <= id; 64 candidates a step
-__device__ __forceinline__ int find_seq(const RaggedArgs &r, int run, int64_t id) {
-    const int lane = threadIdx.x & 63;
-    int lo = 0, n = r.N;
-    while (n > 1) {
-        const int step = (n + 63) / 64, i = lo + lane * step;
-        const bool in = lane * step < n && clamp_row(r.cu[lane * step < n ? i : lo], r.T) / run + i <= id;
-        const int m = __popcll(__ballot(in));
-        const int at = m > 0 ? (m - 1) * step : 0;
-        lo += at;
-        n = n - at < step ? n - at : step;
-    }
-    return __builtin_amdgcn_readfirstlane(lo);
-}
 
 template <bool SILU>
 __device__ __forceinline__ float conv_act(float u) {
@@ -183,7 +150,7 @@ __global__ void __launch_bounds__(CR_NT) k_conv_ragged(ConvRaggedArgs a) {
     const int64_t id = blockIdx.x / nb;
     const int i = find_seq(a.r, a.run, id);
     const Seq sq = seq_of(a.r, i);
-    const int64_t t0 = (id - (sq.begin / a.run + i)) * a.run, n = sq.end - sq.begin;
+    const int64_t t0 = (id - first_run(sq, a.run, i)) * a.run, n = sq.end - sq.begin;
     if (t0 < 0 || t0 >= n || sq.slot < 0 || c0 >= a.C) return;
     const int64_t t1 = t0 + a.run < n ? t0 + a.run : n;
     const T *x = (const T *)a.x + sq.begin * a.sx_t + c0;

@@ -115,7 +115,7 @@ int main() {
     REFUSED(Gdn, run, SF_E_ALIAS, c.state = (float *)c.k)
     REFUSED(Gdn, run, SF_E_ALIAS, c.state = (float *)c.b.slot)
     REFUSED(Gdn, run, SF_E_UNSUPPORTED, c.b.N = INT_MAX; c.s.Hv = 400; c.s.sv_h = c.s.sg_h = 0; c.b.slot = (const int32_t *)P(30);
-            c.s.so_t = 400 * 128; c.s.ss = 400 * 128 * 128; c.b.fresh = nullptr)
+            c.s.so_t = 400 * 128; c.s.ss = 400 * 128 * 128; c.b.fresh = nullptr; c.b.max_len = 1)
     {
         sf_tuning t;
         std::memset(&t, 0, sizeof t);
@@ -201,6 +201,31 @@ int main() {
     REFUSED(Gdn, run, SF_OK, c.b.n_slots = 1; c.s.ss = 0)
     EXPECT(rec.gdn.size() == 3 && rec.gdn[0].Hv == 8 && rec.gdn[0].r.N == 3 && rec.gdn[1].sq_t == 0);
     EXPECT(sf::gdn_token_waves(rec.gdn[0]) == 3 * 8 * 4);
+    // long sequences: a system of every chunk and head in the workspace
+    EXPECT(rec.prep.size() == 3 && rec.walk.size() == 3 && rec.prep[0].n_chunks == 100 / 64 + 3);
+    {
+        Gdn c;
+        const size_t need = sf_gdn_ragged_workspace_bytes(&c.s, &c.b);
+        EXPECT(need == (size_t)4 * 8 * sf::RAG_SYS);
+        c.ws_bytes = need;
+        EXPECT(c.run() == SF_OK);
+        c.ws_bytes = need - 1;
+        EXPECT(c.run() == SF_E_WORKSPACE);
+        c.ws_bytes = need, c.ws = (char *)c.ws + 8;
+        EXPECT(c.run() == SF_E_ALIGN);
+        c.ws = c.o;
+        EXPECT(c.run() == SF_E_ALIAS);
+        c.ws = nullptr;
+        EXPECT(c.run() == SF_E_WORKSPACE);
+        c.b.max_len = sf::RAG_LONG;  // token by token: no workspace
+        EXPECT(sf_gdn_ragged_workspace_bytes(&c.s, &c.b) == 0 && c.run() == SF_OK);
+        c.b.max_len = 90, c.s.io_dtype = SF_F32;
+        EXPECT(sf_gdn_ragged_workspace_bytes(&c.s, &c.b) == 0 && c.run() == SF_OK);
+        EXPECT(rec.prep.size() == 4 && rec.gdn.size() == 6 && rec.gdn[5].longer == 0);
+    }
+    // chunk numbers stay below n_chunks whatever the bounds, decreasing ones too
+    for (int b = 0; b <= 200; ++b)
+        for (int e = b + 1; e <= 200; ++e) EXPECT(b / 64 + 4 + (e - b + 63) / 64 <= 200 / 64 + 5);
     REFUSED(Conv, run, SF_OK, )
     REFUSED(Conv, run, SF_OK, c.s.W = 1; c.tails = nullptr; c.s.ss = 0)
     for (const auto &a : rec.conv)  // every run of every sequence has a number below n_runs

@@ -18,6 +18,14 @@ hipError_t launch_gdn_tokens(const GdnRaggedArgs &a, hipStream_t, hipEvent_t, hi
     record("launch_gdn_tokens").gdn.push_back(a);
     return hipSuccess;
 }
+hipError_t launch_gdn_chunk_prep(const GdnRaggedArgs &a, hipStream_t, hipEvent_t, hipEvent_t) {
+    record("launch_gdn_chunk_prep").prep.push_back(a);
+    return hipSuccess;
+}
+hipError_t launch_gdn_chunk_walk(const GdnRaggedArgs &a, hipStream_t, hipEvent_t, hipEvent_t) {
+    record("launch_gdn_chunk_walk").walk.push_back(a);
+    return hipSuccess;
+}
 hipError_t launch_conv_ragged(const ConvRaggedArgs &a, hipStream_t, hipEvent_t, hipEvent_t) {
     record("launch_conv_ragged").conv.push_back(a);
     return hipSuccess;

@@ -8,7 +8,7 @@
 
 namespace sf {
 struct ServeRecord {
-    std::vector<GdnRaggedArgs> gdn;
+    std::vector<GdnRaggedArgs> gdn, prep, walk;
     std::vector<ConvRaggedArgs> conv;
     std::vector<std::pair<bool, QkArgs>> qk;
 };

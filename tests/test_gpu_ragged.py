@@ -125,27 +125,33 @@ def test_gdn_rows_outside(max_len):
     run_gdn(args, cu, max_len=max_len)
 
 
-@pytest.mark.parametrize("cu", [[0, 200, 90, 150], [-7, 40, 40, 1000], [150, 100, 50, 0], [400, 500, 600, 700]])
-def test_gdn_bad_bounds(cu):
-    """Entries outside [0, T] count as the nearer end, sequences that end before they
-    begin as empty (sequences here may share rows, so o is compared row by row only
-    where one sequence owns them)."""
-    T = 150
+@pytest.mark.parametrize("cu", [[-7, 40, 40, 1000], [400, 500, 600, 700], [-90, -80, 30, 150]])
+def test_gdn_bounds_outside(cu):
+    """Entries outside [0, T] count as the nearer end."""
     print(f"[gdn ragged] bounds {cu}", flush=True)
-    args = gdn_inputs(T, 1, 1, 64, 64, 3, seed=9)
-    state, o = args[5], torch.full(args[2].shape, 7.0, dtype=torch.bfloat16, device=DEV)
-    owners = np.zeros(T, int)
-    for b, e in zip(cu, cu[1:]):
-        owners[max(b, 0):max(e, 0)] += 1
-    want_o, written, want_S = ref.gdn(*args, cu, None)
     for max_len in (1, 150):
-        S = state.clone()
-        sf.gdn_ragged_fwd(*args[:5], S, i32(cu), max_len=max_len, out=(o, torch.empty(1 << 24, dtype=torch.uint8, device=DEV)))
+        run_gdn(gdn_inputs(150, 1, 1, 64, 64, 3, seed=9), cu, max_len=max_len)
+
+
+@pytest.mark.parametrize("cu", [[0, 200, 90, 150], [150, 100, 50, 0], [2 ** 31 - 1, -2 ** 31, 2 ** 31 - 1, 0],
+                                [130, 0, 150, 20, 70]])
+def test_gdn_decreasing_bounds(cu):
+    """Entries that decrease: rows and slots no sequence names are left alone."""
+    T, N = 150, len(cu) - 1
+    print(f"[gdn ragged] bounds {cu}", flush=True)
+    args = gdn_inputs(T, 1, 2, 64, 64, N + 1, seed=9)
+    at = [min(max(c, 0), T) for c in cu]
+    named = np.zeros(T, bool)
+    for b, e in zip(at, at[1:]):
+        named[b:e] = True
+    for max_len in (1, 150):
+        S, o = args[5].clone(), torch.full(args[2].shape, 7.0, dtype=torch.bfloat16, device=DEV)
+        ws = torch.zeros(1 << 24, dtype=torch.uint8, device=DEV)
+        sf.gdn_ragged_fwd(*args[:5], S, i32(cu), max_len=max_len, out=(o, ws))
         torch.cuda.synchronize()
-        close("state", S, want_S, DELTA)
-        own = torch.tensor(owners == 1, device=DEV)
-        close("o", o[own], want_o[owners == 1], DELTA)
-        assert bool((o[torch.tensor(owners == 0, device=DEV)] == 7).all())
+        assert bool((o[torch.tensor(~named, device=DEV)] == 7).all())
+        idle = [i for i in range(N + 1) if i == N or at[i + 1] <= at[i]]
+        assert torch.equal(S[idle], args[5][idle])
 
 
 def test_gdn_strides_and_broadcast():

@@ -171,8 +171,8 @@ def test_entry_points_under_sanitizers(tmp_path):
 
 
 @pytest.mark.skipif(not os.path.exists(HIPCC), reason="hipcc not available")
-@pytest.mark.parametrize("src", ["sf_ragged.hip", "sf_qk.hip"])
-def test_generated_code(src, tmp_path):
+@pytest.mark.parametrize("src,most", [("sf_ragged.hip", 20), ("sf_qk.hip", 41), ("sf_ragged_chunk.hip", 4)])
+def test_generated_code(src, most, tmp_path):
     """No store over its own address, no scratch memory, nothing read before it is written."""
     out = str(tmp_path / "k.s")
     res = subprocess.run([HIPCC, "--offload-arch=gfx950", "-O3", "-std=c++17", "--cuda-device-only", "-S",
@@ -183,5 +183,5 @@ def test_generated_code(src, tmp_path):
     asm = open(out).read()
     n, bad = overlapping_stores(asm)
     kernels, kept = in_memory(asm)
-    assert kernels > 10 and not kept, kept[:3]
+    assert kernels >= most and not kept, kept[:3]
     assert n > 50 and not bad, bad[:3]

@@ -107,9 +107,11 @@ sf_status check_gdn(const sf_gdn_ragged_shape *s, const sf_ragged *b) {
 }
 
 // Sequences of more than RAG_LONG tokens are taken in chunks where the operands are
-// bf16 and the host knows of such a sequence; fp32 operands go token by token.
+// bf16, the host knows of such a sequence and 64 rows span less than 2 GiB (the walk's
+// offsets inside a chunk are 32 bits); fp32 operands go token by token.
 int gdn_longer(const sf_gdn_ragged_shape &s, const sf_ragged &b) {
-    return s.io_dtype == SF_BF16 && b.max_len > sf::RAG_LONG ? sf::RAG_LONG : 0;
+    const bool near = std::max(s.sq_t, s.sv_t) < (int64_t)1 << 23;
+    return s.io_dtype == SF_BF16 && b.max_len > sf::RAG_LONG && near ? sf::RAG_LONG : 0;
 }
 int64_t gdn_chunks(const sf_ragged &b) { return b.T / 64 + b.N; }
 size_t gdn_ragged_ws_bytes(const sf_gdn_ragged_shape &s, const sf_ragged &b) {
@@ -294,7 +296,7 @@ sf_status sf_gdn_ragged_fwd(const sf_gdn_ragged_shape *shape, const sf_ragged *b
         a.longer = gdn_longer(s, b);
         a.n_chunks = gdn_chunks(b);
         a.ws = (char *)ws;
-        TRY(grid_fits(std::max((double)sf::gdn_token_waves(a), (double)a.n_chunks * s.Hk)));
+        TRY(grid_fits(std::max({(double)sf::gdn_token_waves(a), (double)a.n_chunks * s.Hk, (double)sf::gdn_walk_groups(a, 1)})));
         hipEvent_t e0, e1;
         if (a.longer) {
             take_pair(timing_of(tuning), SF_K_GDN_CHUNK_PREP, e0, e1);

@@ -154,10 +154,16 @@ struct GdnRaggedArgs {
     char *ws;          // chunk systems: [n_chunks][Hv] of RAG_SYS bytes
 };
 // A chunk's triangular system, as operand fragments: T = (I + A)^-1 in three bf16
-// planes (exact), P in two, six fragments of 1 KB a plane (sf_ragged_chunk.hip)
-constexpr int RAG_FRAGS = 6, RAG_TP = 3, RAG_PP = 2, RAG_SYS = (RAG_TP + RAG_PP) * RAG_FRAGS * 1024;
-constexpr int RAG_NW = 4;  // waves of a walk workgroup, 16 value columns each
+// planes (exact), P in two, six fragments of 1 KB a plane, then the chunk's e^b,
+// e^(b_63 - b) and beta (sf_ragged_chunk.hip)
+constexpr int RAG_FRAGS = 6, RAG_TP = 3, RAG_PP = 2, RAG_SYS = ((RAG_TP + RAG_PP) * RAG_FRAGS + 1) * 1024;
 constexpr int RAG_LONG = 16;
+// workgroups of the walk with nc 16-column tiles each: (sequence, value head) pairs in
+// eights, their column blocks
+inline int64_t gdn_walk_groups(const GdnRaggedArgs &a, int nc) {
+    return ((int64_t)a.r.N * a.Hv + 7) / 8 * 8 * (a.Dv / (16 * nc));
+}
+inline int gdn_walk_tiles(const GdnRaggedArgs &a) { return 1; }
 hipError_t launch_gdn_chunk_prep(const GdnRaggedArgs &a, hipStream_t s, hipEvent_t e0, hipEvent_t e1);
 hipError_t launch_gdn_chunk_walk(const GdnRaggedArgs &a, hipStream_t s, hipEvent_t e0, hipEvent_t e1);
 hipError_t launch_gdn_tokens(const GdnRaggedArgs &a, hipStream_t s, hipEvent_t e0, hipEvent_t e1);

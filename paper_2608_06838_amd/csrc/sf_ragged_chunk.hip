@@ -18,12 +18,14 @@
 // the output, which is rounded to bf16, takes two pieces.  Against fp32 matrix
 // instructions that is 3 to 6 instructions at 16 times the rate.
 //
-// State columns never mix, so a wave of the walk owns 16 of them and shares only the
-// staged tiles (K, Q, V, T, P) with its workgroup; U, X and S pass from one product to
-// the next inside registers: the accumulator pairs (2m, 2m + 1) hold, in lane row
-// q = lane / 16, rows 32 m + 8 q .. + 7 of the wave's column lane % 16, the slot order
-// of an operand fragment.  The products that build them read their A rows in that
-// order (fragment row n of tile i is 32 (i / 2) + 8 (n / 4) + 4 (i % 2) + n % 4).
+// State columns never mix, so a workgroup of the walk owns 16 NC of them.  Its four
+// waves share each chunk's chain of products by rows: wave w forms the rows of its 16
+// tokens of K S, Q S, U and O, and keeps a quarter of the state's key rows.  Between
+// the products the operands pass through LDS as their three pieces (S, then X, then U).
+// A wave that kept 16 columns for itself would need no exchange, and took 5.8 us a
+// chunk, most of it waiting on its own chain of 200 matrix instructions: a sequence's
+// chunks follow one another, so the chain is what a long prompt waits for.
+//
 #include "sf_ragged.hpp"
 
 #include <type_traits>
@@ -54,6 +56,24 @@ __device__ __forceinline__ void split3(const float (&x)[8], bf16x8 &hi, bf16x8 &
     hi = __builtin_bit_cast(bf16x8, h);
     mid = __builtin_bit_cast(bf16x8, m);
     lo = __builtin_bit_cast(bf16x8, l);
+}
+__device__ __forceinline__ void split3(const f32x4 &x, bf16x4 &hi, bf16x4 &mid, bf16x4 &lo) {
+    typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
+    const f32x4 z = {0.f, 0.f, 0.f, 0.f};
+    f32x4 r = z, s = z;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        r[e] = x[e] - __uint_as_float(__float_as_uint(x[e]) & 0xffff0000u);
+        s[e] = r[e] - __uint_as_float(__float_as_uint(r[e]) & 0xffff0000u);
+    }
+    auto upper = [](const f32x4 &v) {
+        const u32x2 u = {__builtin_amdgcn_perm(__float_as_uint(v[1]), __float_as_uint(v[0]), 0x07060302u),
+                         __builtin_amdgcn_perm(__float_as_uint(v[3]), __float_as_uint(v[2]), 0x07060302u)};
+        return __builtin_bit_cast(bf16x4, u);
+    };
+    hi = upper(x);
+    mid = upper(r);
+    lo = upper(s);
 }
 __device__ __forceinline__ void split3(const f32x4 &a, const f32x4 &b, bf16x8 &hi, bf16x8 &mid, bf16x8 &lo) {
     const float x[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
@@ -88,6 +108,8 @@ struct RowTile {
         }
     }
 };
+
+constexpr int RAG_GATES = (RAG_TP + RAG_PP) * RAG_FRAGS * 1024;  // where a system's gates begin
 
 // fragment (tt, ks) of a lower triangle: tiles 0, 1 have columns 0..31 only
 __device__ __forceinline__ constexpr int tri_frag(int tt, int ks) { return tt < 2 ? tt : 2 + 2 * (tt - 2) + ks; }
@@ -140,8 +162,13 @@ __global__ void __launch_bounds__(256) k_rag_prep(GdnRaggedArgs a) {
         if (w == 0) {
             const bool in = lane < m;
             const int64_t go = (row0 + lane) * a.sg_t + hv * a.sg_h;
-            sb[lane] = wave_scan_dpp(in ? gate_log2(a.g[go]) : 0.f);
-            sbeta[lane] = in ? a.beta[go] : 0.f;
+            const float b = wave_scan_dpp(in ? gate_log2(a.g[go]) : 0.f), be = in ? a.beta[go] : 0.f;
+            sb[lane] = b;
+            sbeta[lane] = be;
+            float *const gates = reinterpret_cast<float *>(a.ws + (id * a.Hv + hv) * (int64_t)RAG_SYS + RAG_GATES) + lane;
+            gates[0] = fexp2(b);
+            gates[64] = fexp2(lane_value(b, 63) - b);
+            gates[128] = be;
         }
         __syncthreads();
         __bf16 *const sys = reinterpret_cast<__bf16 *>(a.ws + (id * a.Hv + hv) * (int64_t)RAG_SYS);
@@ -222,11 +249,11 @@ __global__ void __launch_bounds__(256) k_rag_prep(GdnRaggedArgs a) {
             }
         }
         __syncthreads();
-        // fragments of tile w: rows in the walk's order, columns 32 ks + 8 q4 ..
+        // fragments of tile w: rows 16 w + n16, columns 32 ks + 8 q4 ..
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks) {
             if (ks > (w >> 1)) continue;
-            const float *p = &sT[(32 * (w >> 1) + ar + 4 * (w & 1)) * LA + 32 * ks + 8 * q4];
+            const float *p = &sT[tok * LA + 32 * ks + 8 * q4];
             bf16x8 f[3];
             split3(*reinterpret_cast<const f32x4 *>(p), *reinterpret_cast<const f32x4 *>(p + 4), f[0], f[1], f[2]);
 #pragma unroll
@@ -237,176 +264,259 @@ __global__ void __launch_bounds__(256) k_rag_prep(GdnRaggedArgs a) {
 }
 
 // ----------------------------------------------------------------------- the walk
-template <int DK, int NW>
-__global__ void __launch_bounds__(64 * NW, 2) k_rag_walk(GdnRaggedArgs a) {
-    constexpr int NT = 64 * NW, NK = DK / 16, LD = DK + 16, SW = swx<__bf16, DK>();
-    constexpr int VW = 16 * NW, LDV = VW + 16, SWV = NW == 2 ? 16 : 32;
-    constexpr int BLK = RAG_SYS / 16, SYS = (BLK + NT - 1) / NT;  // 16-byte blocks of a system, of a thread
-    __shared__ __attribute__((aligned(16))) __bf16 sK[64 * LD], sQ[64 * LD], sV[64 * LDV];
-    __shared__ __attribute__((aligned(16))) u32x4 sS[BLK];
-    __shared__ __attribute__((aligned(16))) float sq[64], se[64], sbeta[64];
+// Per chunk, with barriers between the phases:
+//   S's pieces to LDS | K S, Q S of the wave's tokens, X = beta (V - e^b K S) to LDS |
+//   U = T X, to LDS in three pieces times e^(b_63 - b) and as a pair | O, S
+// K, Q, T and P are needed by one wave each, in fragment order: they come from memory
+// into registers a chunk ahead and pass LDS only where K is read transposed.
+// Everything a chunk loads is waited for at one place, before the last chunk's outputs
+// are stored: loads and stores share a counter (see vm_wait_all).
+template <int DK, int NC>
+__global__ void __launch_bounds__(256, 2) k_rag_walk(GdnRaggedArgs a) {
+    constexpr int NK = DK / 32, NS = DK / 64;              // k-steps; state tiles of a wave
+    constexpr int LD = DK + 16, SW = swx<__bf16, DK>();    // K tile
+    constexpr int CW = 16 * NC, LS = DK + 16, LT = 64 + 16;  // pieces [column][row], pitches
+    // NC >= 2: K's tile and U's pieces lie where S's pieces were, so that two workgroups
+    // share a CU; one barrier more keeps the next chunk's S behind their last reads
+    constexpr bool ALIAS = NC >= 2;
+    constexpr int NSP = 3 * CW * LS, NX = 3 * CW * LT, NU = 5 * CW * LT, NKT = 64 * LD;
+    __shared__ __attribute__((aligned(16))) __bf16 mem[NX + (ALIAS ? (NSP > NU + NKT ? NSP : NU + NKT) : NSP + NU + NKT)];
+    __bf16 *const sX = mem, *const sS = mem + NX, *const sU = ALIAS ? sS : sS + NSP, *const sK = sU + NU;
     const int tid = threadIdx.x, lane = tid & 63, q4 = lane >> 4, n16 = lane & 15;
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int ncb = a.Dv / VW;
-    const int cb = blockIdx.x % ncb, h = (blockIdx.x / ncb) % a.Hv, i = blockIdx.x / ncb / a.Hv;
+    // (sequence, value head) pairs eight at a time, their column blocks eight apart: the
+    // blocks of a pair run on one XCD, whose L2 then holds what they share
+    const int ncb = a.Dv / CW;
+    const int64_t pair = ((int64_t)blockIdx.x / (8 * ncb)) * 8 + blockIdx.x % 8;
+    const int cb = (int)(blockIdx.x / 8 % ncb), h = (int)(pair % a.Hv), i = (int)(pair / a.Hv);
+    if (i >= a.r.N) return;
     const Seq s = seq_of(a.r, i);
     const int64_t n = s.end - s.begin;
     if (n <= a.longer || s.slot < 0) return;
-    const int hk = h / (a.Hv / a.Hk), col = cb * VW + 16 * w + n16;
-    const __bf16 *K = (const __bf16 *)a.k + s.begin * a.sq_t + hk * a.sq_h;
-    const __bf16 *Q = (const __bf16 *)a.q + s.begin * a.sq_t + hk * a.sq_h;
-    const __bf16 *V = (const __bf16 *)a.v + s.begin * a.sv_t + h * a.sv_h + cb * VW;
-    __bf16 *O = (__bf16 *)a.o + s.begin * a.so_t + h * a.so_h + cb * VW + 16 * w + 4 * q4;
-    const float *G = a.g + s.begin * a.sg_t + h * a.sg_h, *BE = a.beta + s.begin * a.sg_t + h * a.sg_h;
-    const char *sys = a.ws + (first_run(s, 64, i) * a.Hv + h) * (int64_t)RAG_SYS;
-    float *const st = a.state + s.slot * a.ss + (int64_t)h * DK * a.Dv + col;
+    const int hk = h / (a.Hv / a.Hk), tok = 16 * w + n16;
+    // bases are uniform, a chunk's rows 32-bit offsets from them
+    const char *const K = (const char *)a.k + 2 * (s.begin * a.sq_t + hk * a.sq_h);
+    const char *const Q = (const char *)a.q + 2 * (s.begin * a.sq_t + hk * a.sq_h);
+    const char *const V = (const char *)a.v + 2 * (s.begin * a.sv_t + h * a.sv_h + cb * CW);
+    __bf16 *const O = (__bf16 *)a.o + (s.begin + tok) * a.so_t + h * a.so_h + cb * CW + 4 * q4;
+    const char *const sys = a.ws + (first_run(s, 64, i) * a.Hv + h) * (int64_t)RAG_SYS;
+    const int64_t sys_step = (int64_t)a.Hv * RAG_SYS;
+    float *const st = a.state + s.slot * a.ss + (int64_t)h * DK * a.Dv + (int64_t)(16 * NS * w + 4 * q4) * a.Dv + cb * CW + n16;
 
-    // S[t][r] = state row 32 (t / 2) + 8 q4 + 4 (t % 2) + r, column col
-    auto row = [&](int t, int r) { return 32 * (t >> 1) + 8 * q4 + 4 * (t & 1) + r; };
-    f32x4 S[NK];
+    // S[t][c][r] = state row 16 (NS w + t) + 4 q4 + r, column 16 c + n16 of the block
+    f32x4 S[NS][NC];
     const bool fresh = a.r.fresh && a.r.fresh[i];
 #pragma unroll
-    for (int t = 0; t < NK; ++t)
+    for (int t = 0; t < NS; ++t)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) S[t][r] = fresh ? 0.f : st[(int64_t)row(t, r) * a.Dv];
+        for (int c = 0; c < NC; ++c)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) S[t][c][r] = fresh ? 0.f : st[(int64_t)(16 * t + r) * a.Dv + 16 * c];
 
-    RowTile<DK, NT, LD, SW> tk, tq;
-    RowTile<VW, NT, LDV, SWV> tv;
-    u32x4 ts[SYS] = {};
-    float gl = 0.f, bl = 0.f;
-    auto fetch = [&](int64_t c) {
-        const int m = n - c < 64 ? (int)(n - c) : 64;
-        tk.load(K + c * a.sq_t, a.sq_t, m, tid);
-        tq.load(Q + c * a.sq_t, a.sq_t, m, tid);
-        tv.load(V + c * a.sv_t, a.sv_t, m, tid);
-        const u32x4 *p = reinterpret_cast<const u32x4 *>(sys + (c / 64) * a.Hv * (int64_t)RAG_SYS) + tid;
+    bf16x8 kf[NK], qf[NK], t0[RAG_TP], t1[RAG_TP], p0[RAG_PP], p1[RAG_PP];
+    unsigned short vf[NC][4];
+    f32x4 eb, ee, be;  // of the wave's rows 16 w + 4 q4 + r
+    float et, gam;     // e^b of token 16 w + n16, of the chunk
+    const bool two = w >= 2;  // the wave's tile of T and P has a second k-step
+    // rows past the sequence's end stand for its last one: their beta is 0, so they
+    // change nothing
+    auto last_row = [&](int64_t c) { return n - c < 64 ? (int)(n - c) - 1 : 63; };
+    auto fetch_k = [&](int64_t c) {
+        const char *const p = K + 2 * c * a.sq_t;
+        const uint32_t o = 2u * ((uint32_t)min(tok, last_row(c)) * (uint32_t)a.sq_t + 8 * q4);
 #pragma unroll
-        for (int j = 0; j < SYS; ++j)
-            if (j * NT + NT <= BLK || j * NT + tid < BLK) ts[j] = p[j * NT];
-        if (w == 0) {
-            gl = lane < m ? gate_log2(G[(c + lane) * a.sg_t]) : 0.f;
-            bl = lane < m ? BE[(c + lane) * a.sg_t] : 0.f;
+        for (int ks = 0; ks < NK; ++ks) kf[ks] = *reinterpret_cast<const bf16x8 *>(p + o + 64 * ks);
+    };
+    auto fetch_qv = [&](int64_t c) {
+        const char *const p = Q + 2 * c * a.sq_t, *const v = V + 2 * c * a.sv_t;
+        const uint32_t o = 2u * ((uint32_t)min(tok, last_row(c)) * (uint32_t)a.sq_t + 8 * q4);
+#pragma unroll
+        for (int ks = 0; ks < NK; ++ks) qf[ks] = *reinterpret_cast<const bf16x8 *>(p + o + 64 * ks);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const uint32_t ov = 2u * ((uint32_t)min(16 * w + 4 * q4 + r, last_row(c)) * (uint32_t)a.sv_t + n16);
+#pragma unroll
+            for (int x = 0; x < NC; ++x) vf[x][r] = *reinterpret_cast<const unsigned short *>(v + ov + 32 * x);
         }
     };
-    fetch(0);
-    const LaneOff swo = swz_off<__bf16, LD, SW>(lane), tr8 = tr_off8<__bf16, LD, SW>(lane);
-    const LaneOff trv = tr_off<__bf16, LDV, SWV>(lane);
-    const int ar = 8 * (n16 >> 2) + (n16 & 3), sgn = ((n16 >> 2) & 1) * SW;
-    const bf16x8 *const T = reinterpret_cast<const bf16x8 *>(sS) + lane;
-    const bf16x8 *const P = T + RAG_TP * RAG_FRAGS * 64;
-    for (int64_t c = 0; c < n; c += 64) {
-        __syncthreads();  // the last chunk is done with the tiles
-        tk.store(sK, tid);
-        tq.store(sQ, tid);
-        tv.store(sV, tid);
+    const int f0 = tri_frag(w, 0) * 1024;
+    const uint32_t l16 = 16 * lane;
+    auto fetch_t = [&](const char *p) {
 #pragma unroll
-        for (int j = 0; j < SYS; ++j)
-            if (j * NT + NT <= BLK || j * NT + tid < BLK) sS[j * NT + tid] = ts[j];
-        if (w == 0) {
-            const float b = wave_scan_dpp(gl);
-            sq[lane] = fexp2(b);
-            se[lane] = fexp2(lane_value(b, 63) - b);
-            sbeta[lane] = bl;
+        for (int pl = 0; pl < RAG_TP; ++pl) t0[pl] = *reinterpret_cast<const bf16x8 *>(p + f0 + pl * RAG_FRAGS * 1024 + l16);
+        if (two) {
+#pragma unroll
+            for (int pl = 0; pl < RAG_TP; ++pl)
+                t1[pl] = *reinterpret_cast<const bf16x8 *>(p + f0 + (pl * RAG_FRAGS + 1) * 1024 + l16);
+        }
+    };
+    auto fetch_p = [&](const char *p) {
+        p += RAG_TP * RAG_FRAGS * 1024;
+#pragma unroll
+        for (int pl = 0; pl < RAG_PP; ++pl) p0[pl] = *reinterpret_cast<const bf16x8 *>(p + f0 + pl * RAG_FRAGS * 1024 + l16);
+        if (two) {
+#pragma unroll
+            for (int pl = 0; pl < RAG_PP; ++pl)
+                p1[pl] = *reinterpret_cast<const bf16x8 *>(p + f0 + (pl * RAG_FRAGS + 1) * 1024 + l16);
+        }
+    };
+    auto fetch_gates = [&](const char *p) {
+        p += RAG_GATES + 64 * w;
+        eb = *reinterpret_cast<const f32x4 *>(p + 16 * q4);
+        ee = *reinterpret_cast<const f32x4 *>(p + 256 + 16 * q4);
+        be = *reinterpret_cast<const f32x4 *>(p + 512 + 16 * q4);
+        et = *reinterpret_cast<const float *>(p + 4 * n16);
+        gam = *reinterpret_cast<const float *>(p - 64 * w + 4 * 63);
+    };
+    const bf16x8 zero8 = __builtin_bit_cast(bf16x8, u32x4{0u, 0u, 0u, 0u});
+#pragma unroll
+    for (int pl = 0; pl < RAG_TP; ++pl) t1[pl] = zero8;
+#pragma unroll
+    for (int pl = 0; pl < RAG_PP; ++pl) p1[pl] = zero8;
+    fetch_k(0);
+    fetch_qv(0);
+    fetch_t(sys);
+    fetch_p(sys);
+    fetch_gates(sys);
+    const LaneOff tr = tr_off<__bf16, LD, SW>(lane);
+    bf16x4 out[NC];
+    const char *next = sys;
+    for (int64_t c = 0; c < n; c += 64) {
+        next += sys_step;
+        const bool more = c + 64 < n;
+        if (ALIAS && c > 0) __syncthreads();  // the last chunk is done with K and U
+        // S's pieces, [piece][column][key row]
+#pragma unroll
+        for (int x = 0; x < NC; ++x)
+#pragma unroll
+            for (int t = 0; t < NS; ++t) {
+                bf16x4 f[3];
+                split3(S[t][x], f[0], f[1], f[2]);
+#pragma unroll
+                for (int p = 0; p < 3; ++p)
+                    *reinterpret_cast<bf16x4 *>(sS + (p * CW + 16 * x + n16) * LS + 16 * (NS * w + t) + 4 * q4) = f[p];
+            }
+        vm_wait_all();
+        if (c > 0) {
+#pragma unroll
+            for (int x = 0; x < NC; ++x) *reinterpret_cast<bf16x4 *>(O + (c - 64) * a.so_t + 16 * x) = out[x];
         }
         __syncthreads();
-        if (c + 64 < n) fetch(c + 64);
-
-        f32x4 X[4], Y[4];  // K S (rows: tokens), (Q S)^T (columns: tokens)
+        f32x4 X[NC], Y[NC];  // K S (rows: tokens 16 w + 4 q4 + r), (Q S)^T (columns: tokens 16 w + n16)
 #pragma unroll
-        for (int t = 0; t < 4; ++t) X[t] = Y[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int x = 0; x < NC; ++x) X[x] = Y[x] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int ks = 0; ks < DK / 32; ++ks) {
-            bf16x8 f[3];
-            split3(S[2 * ks], S[2 * ks + 1], f[0], f[1], f[2]);
+        for (int x = 0; x < NC; ++x)
 #pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                const bf16x8 kf = *reinterpret_cast<const bf16x8 *>(
-                    &sK[(ar + 32 * (t >> 1) + 4 * (t & 1)) * LD + 8 * q4 + 32 * ks + (((32 * ks) & SW) ? -sgn : sgn)]);
-                mma(X[t], kf, f[2]);
-                mma(X[t], kf, f[1]);
-                mma(X[t], kf, f[0]);
-                const bf16x8 qf = ldfrag_swz<__bf16, LD, SW>(sQ, swo, 16 * t, 32 * ks);
-                mma(Y[t], f[2], qf);
-                mma(Y[t], f[1], qf);
-                mma(Y[t], f[0], qf);
-            }
+            for (int p = 2; p >= 0; --p)
+#pragma unroll
+                for (int ks = 0; ks < NK; ++ks) {
+                    const bf16x8 f = *reinterpret_cast<const bf16x8 *>(sS + (p * CW + 16 * x + n16) * LS + 32 * ks + 8 * q4);
+                    mma(X[x], kf[ks], f);
+                    mma(Y[x], f, qf[ks]);
+                }
+#pragma unroll
+        for (int x = 0; x < NC; ++x) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                X[x][r] = be[r] * (__uint_as_float((unsigned)vf[x][r] << 16) - eb[r] * X[x][r]);
+            bf16x4 f[3];
+            split3(X[x], f[0], f[1], f[2]);
+#pragma unroll
+            for (int p = 0; p < 3; ++p)
+                *reinterpret_cast<bf16x4 *>(sX + (p * CW + 16 * x + n16) * LT + 16 * w + 4 * q4) = f[p];
         }
-        // X = beta (V - e^b K S); the transposing read returns V in X's own slots
+        if (more) fetch_qv(c + 64);
+        __syncthreads();
+        // K's tile, for the transposed reads (S's pieces have had their last read)
 #pragma unroll
-        for (int ks = 0; ks < 2; ++ks) {
-            const bf16x8 vf = ldfragTR<__bf16, LDV, SWV>(sV, trv, 32 * ks, 16 * w);
+        for (int ks = 0; ks < NK; ++ks)
+            *reinterpret_cast<bf16x8 *>(sK + tok * LD + swz_col(tok, 32 * ks + 8 * q4, SW)) = kf[ks];
+        if (more) fetch_k(c + 64);
+        f32x4 U[NC];
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const int t = 2 * ks + u;
-                const f32x4 eb = *reinterpret_cast<const f32x4 *>(&sq[row(t, 0)]);
-                const f32x4 be = *reinterpret_cast<const f32x4 *>(&sbeta[row(t, 0)]);
+        for (int x = 0; x < NC; ++x) {
+            U[x] = f32x4{0.f, 0.f, 0.f, 0.f};
+            f32x4 U1 = U[x];
 #pragma unroll
-                for (int r = 0; r < 4; ++r) X[t][r] = be[r] * ((float)vf[4 * u + r] - eb[r] * X[t][r]);
+            for (int ks = 0; ks < 2; ++ks) {
+                if (ks == 1 && !two) continue;
+                const bf16x8(&t)[RAG_TP] = ks ? t1 : t0;
+                bf16x8 f[3];
+#pragma unroll
+                for (int p = 0; p < 3; ++p)
+                    f[p] = *reinterpret_cast<const bf16x8 *>(sX + (p * CW + 16 * x + n16) * LT + 32 * ks + 8 * q4);
+                mma(U1, t[2], f[0]);
+                mma(U[x], t[1], f[1]);
+                mma(U1, t[0], f[2]);
+                mma(U[x], t[1], f[0]);
+                mma(U1, t[0], f[1]);
+                mma(U[x], t[0], f[0]);
             }
-        }
-        f32x4 U[4];
+            U[x] += U1;
+            bf16x4 f[5];
+            const f32x4 ue = U[x] * ee;
+            split3(ue, f[0], f[1], f[2]);
 #pragma unroll
-        for (int t = 0; t < 4; ++t) U[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int ks = 0; ks < 2; ++ks) {
-            bf16x8 f[3];
-            split3(X[2 * ks], X[2 * ks + 1], f[0], f[1], f[2]);
-#pragma unroll
-            for (int t = 2 * ks; t < 4; ++t) {
-                const int fr = tri_frag(t, ks) * 64;
-                const bf16x8 t0 = T[fr], t1 = T[fr + RAG_FRAGS * 64], t2 = T[fr + 2 * RAG_FRAGS * 64];
-                mma(U[t], t2, f[0]);
-                mma(U[t], t1, f[1]);
-                mma(U[t], t0, f[2]);
-                mma(U[t], t1, f[0]);
-                mma(U[t], t0, f[1]);
-                mma(U[t], t0, f[0]);
+            for (int r = 0; r < 4; ++r) {
+                f[3][r] = (__bf16)U[x][r];
+                f[4][r] = (__bf16)(U[x][r] - (float)f[3][r]);
             }
+#pragma unroll
+            for (int p = 0; p < 5; ++p)
+                *reinterpret_cast<bf16x4 *>(sU + (p * CW + 16 * x + n16) * LT + 16 * w + 4 * q4) = f[p];
         }
+        if (more) fetch_t(next);
+        __syncthreads();
         // O^T = e^b (Q S)^T + U^T P^T
 #pragma unroll
-        for (int t = 0; t < 4; ++t) Y[t] *= sq[16 * t + n16];
+        for (int x = 0; x < NC; ++x) {
+            Y[x] *= et;
 #pragma unroll
-        for (int ks = 0; ks < 2; ++ks) {
-            bf16x8 uh, ul;
-            split_acc<__bf16, true>(U[2 * ks], U[2 * ks + 1], uh, ul);
-#pragma unroll
-            for (int t = 2 * ks; t < 4; ++t) {
-                const int fr = tri_frag(t, ks) * 64;
-                const bf16x8 p0 = P[fr], p1 = P[fr + RAG_FRAGS * 64];
-                mma(Y[t], uh, p1);
-                mma(Y[t], ul, p0);
-                mma(Y[t], uh, p0);
+            for (int ks = 0; ks < 2; ++ks) {
+                if (ks == 1 && !two) continue;
+                const bf16x8 uh = *reinterpret_cast<const bf16x8 *>(sU + (3 * CW + 16 * x + n16) * LT + 32 * ks + 8 * q4);
+                const bf16x8 ul = *reinterpret_cast<const bf16x8 *>(sU + (4 * CW + 16 * x + n16) * LT + 32 * ks + 8 * q4);
+                mma(Y[x], uh, ks ? p1[1] : p0[1]);
+                mma(Y[x], ul, ks ? p1[0] : p0[0]);
+                mma(Y[x], uh, ks ? p1[0] : p0[0]);
             }
-        }
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
-            const int64_t tok = c + 16 * t + n16;
-            if (tok < n) st4(O + tok * a.so_t, Y[t][0], Y[t][1], Y[t][2], Y[t][3]);
+            for (int r = 0; r < 4; ++r) out[x][r] = (__bf16)Y[x][r];
         }
+        if (more) fetch_p(next);
         // S = e^(b_63) S + K^T e^(b_63 - b) U
-        const float gam = sq[63];
 #pragma unroll
-        for (int t = 0; t < NK; ++t) S[t] *= gam;
+        for (int t = 0; t < NS; ++t)
+#pragma unroll
+            for (int x = 0; x < NC; ++x) S[t][x] *= gam;
+        if (more) fetch_gates(next);
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks) {
+            bf16x8 kt[NS];
 #pragma unroll
-            for (int t = 2 * ks; t < 2 * ks + 2; ++t) U[t] *= *reinterpret_cast<const f32x4 *>(&se[row(t, 0)]);
-            bf16x8 f[3];
-            split3(U[2 * ks], U[2 * ks + 1], f[0], f[1], f[2]);
+            for (int t = 0; t < NS; ++t) kt[t] = ldfragTR<__bf16, LD, SW>(sK, tr, 32 * ks, 16 * (NS * w + t));
 #pragma unroll
-            for (int t = 0; t < NK; ++t) {
-                const bf16x8 kf = ldfragTR<__bf16, LD, SW>(sK, tr8, 32 * ks, 32 * (t >> 1) + 4 * (t & 1));
-                mma(S[t], kf, f[2]);
-                mma(S[t], kf, f[1]);
-                mma(S[t], kf, f[0]);
-            }
+            for (int x = 0; x < NC; ++x)
+#pragma unroll
+                for (int p = 2; p >= 0; --p) {
+                    const bf16x8 f = *reinterpret_cast<const bf16x8 *>(sU + (p * CW + 16 * x + n16) * LT + 32 * ks + 8 * q4);
+#pragma unroll
+                    for (int t = 0; t < NS; ++t) mma(S[t][x], kt[t], f);
+                }
         }
     }
+    const int64_t last = (n - 1) / 64 * 64;
+    if (last + tok < n) {
 #pragma unroll
-    for (int t = 0; t < NK; ++t)
+        for (int x = 0; x < NC; ++x) *reinterpret_cast<bf16x4 *>(O + last * a.so_t + 16 * x) = out[x];
+    }
 #pragma unroll
-        for (int r = 0; r < 4; ++r) st[(int64_t)row(t, r) * a.Dv] = S[t][r];
+    for (int t = 0; t < NS; ++t)
+#pragma unroll
+        for (int x = 0; x < NC; ++x)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) st[(int64_t)(16 * t + r) * a.Dv + 16 * x] = S[t][x][r];
 }
 
 }  // namespace
@@ -419,9 +529,14 @@ hipError_t launch_gdn_chunk_prep(const GdnRaggedArgs &a, hipStream_t s, hipEvent
 }
 
 hipError_t launch_gdn_chunk_walk(const GdnRaggedArgs &a, hipStream_t s, hipEvent_t e0, hipEvent_t e1) {
-    const dim3 grid((unsigned)((int64_t)a.r.N * a.Hv * (a.Dv / (16 * RAG_NW)))), block(64 * RAG_NW);
-    if (a.Dk == 128) hipExtLaunchKernelGGL((k_rag_walk<128, RAG_NW>), grid, block, 0, s, e0, e1, 0, a);
-    else hipExtLaunchKernelGGL((k_rag_walk<64, RAG_NW>), grid, block, 0, s, e0, e1, 0, a);
+    auto go = [&](auto nc) {
+        constexpr int NC = decltype(nc)::value;
+        const dim3 grid((unsigned)gdn_walk_groups(a, NC)), block(256);
+        if (a.Dk == 128) hipExtLaunchKernelGGL((k_rag_walk<128, NC>), grid, block, 0, s, e0, e1, 0, a);
+        else hipExtLaunchKernelGGL((k_rag_walk<64, NC>), grid, block, 0, s, e0, e1, 0, a);
+    };
+    if (gdn_walk_tiles(a) == 1) go(std::integral_constant<int, 1>());
+    else go(std::integral_constant<int, 2>());
     return hipGetLastError();
 }
 

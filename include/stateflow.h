@@ -132,12 +132,12 @@ typedef enum {
     SF_K_GDN_DSCAN = 13, /* gated delta rule backward: transposed scan */
     SF_K_GDN_DWALK = 14, /* gated delta rule backward: state-gradient walk */
     SF_K_GDN_DCHUNK = 15, /* gated delta rule backward: per-chunk parameter gradients */
-    SF_K_GDN_TOKENS = 16,  /* ragged gated delta rule: sequences taken token by token */
+    SF_K_GDN_TOKENS = 16,  /* ragged gated delta rule without long sequences: token by token */
     SF_K_CONV_RAGGED = 17, /* ragged short convolution */
     SF_K_QK_FWD = 18,      /* norms and rotation of queries and keys */
     SF_K_QK_BWD = 19,      /* their gradients (dq, dk, weight partials and their sums) */
     SF_K_GDN_CHUNK_PREP = 20, /* ragged gated delta rule: triangular systems of the long sequences' chunks */
-    SF_K_GDN_CHUNK_WALK = 21, /* ragged gated delta rule: walk over those chunks */
+    SF_K_GDN_CHUNK_WALK = 21, /* ragged gated delta rule: walk over those chunks, and the short sequences beside it */
     SF_K_COUNT = 22
 } sf_kernel_id;
 

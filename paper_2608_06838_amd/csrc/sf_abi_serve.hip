@@ -114,8 +114,30 @@ int gdn_longer(const sf_gdn_ragged_shape &s, const sf_ragged &b) {
     return s.io_dtype == SF_BF16 && b.max_len > sf::RAG_LONG && near ? sf::RAG_LONG : 0;
 }
 int64_t gdn_chunks(const sf_ragged &b) { return b.T / 64 + b.N; }
+sf::GdnRaggedArgs gdn_args(const sf_gdn_ragged_shape &s, const sf_ragged &b) {
+    sf::GdnRaggedArgs a{};
+    a.r = ragged_args(b);
+    a.Hk = s.Hk;
+    a.Hv = s.Hv;
+    a.Dk = s.Dk;
+    a.Dv = s.Dv;
+    a.io = s.io_dtype;
+    a.n_cu = device_cus();
+    a.sq_t = s.sq_t;
+    a.sq_h = s.sq_h;
+    a.sv_t = s.sv_t;
+    a.sv_h = s.sv_h;
+    a.so_t = s.so_t;
+    a.so_h = s.so_h;
+    a.sg_t = s.sg_t;
+    a.sg_h = s.sg_h;
+    a.ss = s.ss;
+    a.longer = gdn_longer(s, b);
+    a.n_chunks = gdn_chunks(b);
+    return a;
+}
 size_t gdn_ragged_ws_bytes(const sf_gdn_ragged_shape &s, const sf_ragged &b) {
-    return b.N > 0 && b.T > 0 && gdn_longer(s, b) ? (size_t)gdn_chunks(b) * (size_t)s.Hv * sf::RAG_SYS : 0;
+    return b.N > 0 && b.T > 0 && gdn_longer(s, b) ? sf::gdn_chunk_ws_bytes(gdn_args(s, b)) : 0;
 }
 
 // ------------------------------------------------------------- norms and rotation
@@ -269,8 +291,7 @@ sf_status sf_gdn_ragged_fwd(const sf_gdn_ragged_shape *shape, const sf_ragged *b
                         {strided(o, {{b.T, s.so_t}, {s.Hv, s.so_h}}, s.Dv, e, "o"),
                          pool_range("state", state, b.n_slots, per, s.ss), wsrange(need ? ws : nullptr, need)}));
         if (b.n_slots == 0) return SF_OK;  // every slot is out of range
-        sf::GdnRaggedArgs a{};
-        a.r = ragged_args(b);
+        sf::GdnRaggedArgs a = gdn_args(s, b);
         a.q = q;
         a.k = k;
         a.v = v;
@@ -278,34 +299,20 @@ sf_status sf_gdn_ragged_fwd(const sf_gdn_ragged_shape *shape, const sf_ragged *b
         a.beta = beta;
         a.state = state;
         a.o = o;
-        a.Hk = s.Hk;
-        a.Hv = s.Hv;
-        a.Dk = s.Dk;
-        a.Dv = s.Dv;
-        a.io = s.io_dtype;
-        a.n_cu = device_cus();
-        a.sq_t = s.sq_t;
-        a.sq_h = s.sq_h;
-        a.sv_t = s.sv_t;
-        a.sv_h = s.sv_h;
-        a.so_t = s.so_t;
-        a.so_h = s.so_h;
-        a.sg_t = s.sg_t;
-        a.sg_h = s.sg_h;
-        a.ss = s.ss;
-        a.longer = gdn_longer(s, b);
-        a.n_chunks = gdn_chunks(b);
         a.ws = (char *)ws;
-        TRY(grid_fits(std::max({(double)sf::gdn_token_waves(a), (double)a.n_chunks * s.Hk, (double)sf::gdn_walk_groups(a, 1)})));
+        a.plan = need ? (int32_t *)(a.ws + sf::gdn_plan_at(a)) : nullptr;
+        const double tok = (double)sf::gdn_token_waves(a);
+        TRY(grid_fits(std::max(tok + sf::gdn_walk_groups(a), (double)a.n_chunks * s.Hk + 1)));
+        sf_timing *const tm = timing_of(tuning);
         hipEvent_t e0, e1;
-        if (a.longer) {
-            take_pair(timing_of(tuning), SF_K_GDN_CHUNK_PREP, e0, e1);
-            TRY(launched(sf::launch_gdn_chunk_prep(a, (hipStream_t)stream, e0, e1)));
-            take_pair(timing_of(tuning), SF_K_GDN_CHUNK_WALK, e0, e1);
-            TRY(launched(sf::launch_gdn_chunk_walk(a, (hipStream_t)stream, e0, e1)));
+        if (!a.longer) {
+            take_pair(tm, SF_K_GDN_TOKENS, e0, e1);
+            return launched(sf::launch_gdn_tokens(a, (hipStream_t)stream, e0, e1));
         }
-        take_pair(timing_of(tuning), SF_K_GDN_TOKENS, e0, e1);
-        return launched(sf::launch_gdn_tokens(a, (hipStream_t)stream, e0, e1));
+        take_pair(tm, SF_K_GDN_CHUNK_PREP, e0, e1);
+        TRY(launched(sf::launch_gdn_chunk_prep(a, (hipStream_t)stream, e0, e1)));
+        take_pair(tm, SF_K_GDN_CHUNK_WALK, e0, e1);
+        return launched(sf::launch_gdn_chunk_walk(a, (hipStream_t)stream, e0, e1));
     });
 }
 

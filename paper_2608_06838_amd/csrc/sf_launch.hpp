@@ -152,24 +152,34 @@ struct GdnRaggedArgs {
     int32_t longer;    // sequences of more tokens are taken in chunks (0: none are)
     int64_t n_chunks;  // upper bound of the chunks: T / 64 + N
     char *ws;          // chunk systems: [n_chunks][Hv] of RAG_SYS bytes
+    int32_t *plan;     // [1 + N], see gdn_plan_at
 };
+// waves of the token-by-token kernel: one for each sequence, value head and tile of 4 TOK_CL columns
+constexpr int TOK_CL = 8;
+inline int64_t gdn_token_waves(const GdnRaggedArgs &a) { return (int64_t)a.r.N * a.Hv * (a.Dv / (4 * TOK_CL)); }
 // A chunk's triangular system, as operand fragments: T = (I + A)^-1 in three bf16
 // planes (exact), P in two, six fragments of 1 KB a plane, then the chunk's e^b,
 // e^(b_63 - b) and beta (sf_ragged_chunk.hip)
 constexpr int RAG_FRAGS = 6, RAG_TP = 3, RAG_PP = 2, RAG_SYS = ((RAG_TP + RAG_PP) * RAG_FRAGS + 1) * 1024;
 constexpr int RAG_LONG = 16;
-// workgroups of the walk with nc 16-column tiles each: (sequence, value head) pairs in
-// eights, their column blocks
-inline int64_t gdn_walk_groups(const GdnRaggedArgs &a, int nc) {
-    return ((int64_t)a.r.N * a.Hv + 7) / 8 * 8 * (a.Dv / (16 * nc));
+// items of the walk with nc 16-column tiles each, for n sequences: (sequence, value
+// head) pairs in eights, their column blocks
+__host__ __device__ inline int64_t gdn_walk_items(const GdnRaggedArgs &a, int64_t n, int nc) {
+    return (n * a.Hv + 7) / 8 * 8 * (a.Dv / (16 * nc));
 }
-inline int gdn_walk_tiles(const GdnRaggedArgs &a) { return 1; }
+// workgroups of the walk: an item each while there are fewer than eight a CU
+inline int64_t gdn_walk_groups(const GdnRaggedArgs &a) {
+    const int64_t n = gdn_walk_items(a, a.r.N, 1), most = 8 * (int64_t)a.n_cu;
+    return n < most ? n : most;
+}
+// behind the chunk systems: how many sequences are taken in chunks, then their numbers,
+// longest first
+inline size_t gdn_plan_at(const GdnRaggedArgs &a) { return (size_t)a.n_chunks * (size_t)a.Hv * RAG_SYS; }
+inline size_t gdn_chunk_ws_bytes(const GdnRaggedArgs &a) { return gdn_plan_at(a) + 4 * ((size_t)a.r.N + 1); }
+// T and P of every chunk and the plan; then the walk, with the other sequences' tokens
 hipError_t launch_gdn_chunk_prep(const GdnRaggedArgs &a, hipStream_t s, hipEvent_t e0, hipEvent_t e1);
 hipError_t launch_gdn_chunk_walk(const GdnRaggedArgs &a, hipStream_t s, hipEvent_t e0, hipEvent_t e1);
 hipError_t launch_gdn_tokens(const GdnRaggedArgs &a, hipStream_t s, hipEvent_t e0, hipEvent_t e1);
-// waves of that launch: one for each sequence, value head and tile of 4 TOK_CL columns
-constexpr int TOK_CL = 8;
-inline int64_t gdn_token_waves(const GdnRaggedArgs &a) { return (int64_t)a.r.N * a.Hv * (a.Dv / (4 * TOK_CL)); }
 struct ConvRaggedArgs {
     RaggedArgs r;
     const void *x;

@@ -2,18 +2,8 @@
 // packed along the token axis, each with a state of its own in a pool of slots,
 // updated in place.
 //
-// Gated delta rule, token by token (S <- e^g S, u = beta (v - S^T k), S <- S + k u^T,
-// o = S^T q).  A single token reads and writes the whole state for 6 flops an
-// element: the roofline is HBM.  State columns (value channels) never mix, so a
-// wave owns CW columns of one head of one sequence and keeps them in registers from
-// the sequence's first token to its last; no LDS, no barrier.  Lane (rg, cl) holds
-// rows rg RPL .. + RPL - 1 of columns 4 cl .. + 3: a row's columns are 16 bytes of
-// 8 consecutive lanes, one 128-byte line, and k and q come as the lane's own run of
-// rows, one or two 16-byte loads that its neighbours share.  With a = e^g and the old
-// state S,
-//     S^T k and S^T q are summed together,   u = beta (v - a S^T k),
-//     o = a S^T q + (k . q) u,               S <- a S + k u^T,
-// so a token costs one reduction over the row groups, of nine sums.
+// Gated delta rule: sequences taken token by token (gdn_tokens, sf_ragged.hpp); long
+// ones are taken in chunks by sf_ragged_chunk.hip.  Short convolution: below.
 #include "sf_ragged.hpp"
 
 #include <type_traits>
@@ -23,99 +13,16 @@ namespace sf {
 namespace {
 
 // ------------------------------------------------- gated delta rule, token by token
-constexpr int TOK_NT = 256;
-
-// sum over the row groups (lanes that differ in the bits from CL up), in every lane
-template <int CL>
-__device__ __forceinline__ float group_sum(float x) {
-    static_assert(CL == 4 || CL == 8, "column lanes");
-    x += dpp_or0<0x128>(x);                       // row_ror:8
-    if constexpr (CL == 4) x += dpp_or0<0x124>(x);  // row_ror:4
-    return sum_rows(x);
-}
-
-template <typename T, int N> struct Vec { typedef T type __attribute__((ext_vector_type(N))); };
-
-template <typename T, int DK, int CL>
+template <typename T, int DK>
 __global__ void __launch_bounds__(TOK_NT) k_gdn_tokens(GdnRaggedArgs a) {
-    constexpr int CW = 4 * CL, RG = 64 / CL, RPL = DK / RG;
-    typedef typename Vec<T, RPL>::type rows_t;
-    typedef typename Vec<T, 4>::type cols_t;
-    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int nt = a.Dv / CW;
-    const int64_t unit = (int64_t)blockIdx.x * (TOK_NT / 64) + w;
-    const int tile = (int)(unit % nt);
-    const int64_t ih = unit / nt;
-    const int h = (int)(ih % a.Hv);
-    const int64_t i = ih / a.Hv;
-    if (i >= a.r.N) return;
-    const Seq sq = seq_of(a.r, (int)i);
-    if (sq.end <= sq.begin || sq.slot < 0 || (a.longer && sq.end - sq.begin > a.longer)) return;
-    const int rg = lane / CL, col = tile * CW + 4 * (lane % CL), hk = h / (a.Hv / a.Hk);
-    float *const sp = a.state + sq.slot * a.ss + (int64_t)h * DK * a.Dv + (int64_t)rg * RPL * a.Dv + col;
-    f32x4 S[RPL];
-    const bool fresh = a.r.fresh && a.r.fresh[i];
-#pragma unroll
-    for (int m = 0; m < RPL; ++m) S[m] = fresh ? f32x4{0.f, 0.f, 0.f, 0.f} : *reinterpret_cast<const f32x4 *>(sp + (int64_t)m * a.Dv);
-    const T *kp = (const T *)a.k + hk * a.sq_h + rg * RPL, *qp = (const T *)a.q + hk * a.sq_h + rg * RPL;
-    const T *vp = (const T *)a.v + h * a.sv_h + col;
-    T *op = (T *)a.o + h * a.so_h + col;
-    const float *gp = a.g + h * a.sg_h, *bp = a.beta + h * a.sg_h;
-    rows_t kn = *reinterpret_cast<const rows_t *>(kp + sq.begin * a.sq_t);
-    rows_t qn = *reinterpret_cast<const rows_t *>(qp + sq.begin * a.sq_t);
-    cols_t vn = *reinterpret_cast<const cols_t *>(vp + sq.begin * a.sv_t);
-    float gn = gp[sq.begin * a.sg_t], bn = bp[sq.begin * a.sg_t];
-    for (int64_t t = sq.begin; t < sq.end; ++t) {
-        const rows_t kt = kn, qt = qn;
-        const cols_t vt = vn;
-        const float al = fexp2(gn * LOG2E), be = bn;
-        if (t + 1 < sq.end) {  // the next token's, a step ahead
-            kn = *reinterpret_cast<const rows_t *>(kp + (t + 1) * a.sq_t);
-            qn = *reinterpret_cast<const rows_t *>(qp + (t + 1) * a.sq_t);
-            vn = *reinterpret_cast<const cols_t *>(vp + (t + 1) * a.sv_t);
-            gn = gp[(t + 1) * a.sg_t];
-            bn = bp[(t + 1) * a.sg_t];
-        }
-        f32x4 sk = {0.f, 0.f, 0.f, 0.f}, sv = sk;
-        float kq = 0.f;
-#pragma unroll
-        for (int m = 0; m < RPL; ++m) {
-            const float km = (float)kt[m], qm = (float)qt[m];
-            kq = fmaf(km, qm, kq);
-#pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                sk[c] = fmaf(S[m][c], km, sk[c]);
-                sv[c] = fmaf(S[m][c], qm, sv[c]);
-            }
-        }
-        kq = group_sum<CL>(kq);
-        f32x4 u = {0.f, 0.f, 0.f, 0.f}, o = u;
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-            u[c] = be * ((float)vt[c] - al * group_sum<CL>(sk[c]));
-            o[c] = fmaf(kq, u[c], al * group_sum<CL>(sv[c]));
-        }
-#pragma unroll
-        for (int m = 0; m < RPL; ++m) {
-            const float km = (float)kt[m];
-#pragma unroll
-            for (int c = 0; c < 4; ++c) S[m][c] = fmaf(km, u[c], al * S[m][c]);
-        }
-        if (rg == 0) {
-            T *p = op + t * a.so_t;
-            if constexpr (sizeof(T) == 2) st4(p, o[0], o[1], o[2], o[3]);
-            else *reinterpret_cast<f32x4 *>(p) = o;
-        }
-    }
-#pragma unroll
-    for (int m = 0; m < RPL; ++m) *reinterpret_cast<f32x4 *>(sp + (int64_t)m * a.Dv) = S[m];
+    gdn_tokens<T, DK, TOK_CL>(a, (int64_t)blockIdx.x * (TOK_NT / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6));
 }
 
 template <typename T>
 hipError_t gdn_tokens_t(const GdnRaggedArgs &a, hipStream_t s, hipEvent_t e0, hipEvent_t e1) {
     const dim3 grid((unsigned)((gdn_token_waves(a) + TOK_NT / 64 - 1) / (TOK_NT / 64)));
-    if (a.Dk == 128) hipExtLaunchKernelGGL((k_gdn_tokens<T, 128, TOK_CL>), grid, dim3(TOK_NT), 0, s, e0, e1, 0, a);
-    else hipExtLaunchKernelGGL((k_gdn_tokens<T, 64, TOK_CL>), grid, dim3(TOK_NT), 0, s, e0, e1, 0, a);
+    if (a.Dk == 128) hipExtLaunchKernelGGL((k_gdn_tokens<T, 128>), grid, dim3(TOK_NT), 0, s, e0, e1, 0, a);
+    else hipExtLaunchKernelGGL((k_gdn_tokens<T, 64>), grid, dim3(TOK_NT), 0, s, e0, e1, 0, a);
     return hipGetLastError();
 }
 

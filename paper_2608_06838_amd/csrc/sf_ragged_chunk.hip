@@ -85,7 +85,7 @@ __device__ __forceinline__ void split3(const f32x4 &a, const f32x4 &b, bf16x8 &h
 __device__ __forceinline__ float gate_log2(float g) { return fmaxf(g, -104.f) * LOG2E; }
 
 // Rows [0, 64) of a chunk tile of D channels, in 16-byte blocks over NT threads, rows
-// from m on zero; to LDS with pitch LD, rows of bit 3 swizzled by SW channels (see
+// from m on the last one again; to LDS with pitch LD, rows of bit 3 swizzled by SW channels (see
 // ldfragTR).
 template <int D, int NT, int LD, int SW>
 struct RowTile {
@@ -95,9 +95,8 @@ struct RowTile {
     __device__ __forceinline__ void load(const __bf16 *p, int64_t ld, int m, int tid) {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const int row = tid / BPR + RPP * i;
-            r[i] = u32x4{0u, 0u, 0u, 0u};
-            if (row < m) r[i] = *reinterpret_cast<const u32x4 *>(p + row * ld + 8 * (tid % BPR));
+            const int row = min(tid / BPR + RPP * i, m - 1);
+            r[i] = *reinterpret_cast<const u32x4 *>(p + row * ld + 8 * (tid % BPR));
         }
     }
     __device__ __forceinline__ void store(__bf16 *lds, int tid) const {
@@ -114,28 +113,80 @@ constexpr int RAG_GATES = (RAG_TP + RAG_PP) * RAG_FRAGS * 1024;  // where a syst
 // fragment (tt, ks) of a lower triangle: tiles 0, 1 have columns 0..31 only
 __device__ __forceinline__ constexpr int tri_frag(int tt, int ks) { return tt < 2 ? tt : 2 + 2 * (tt - 2) + ks; }
 
+// The sequences that are taken in chunks, longest first: the walk's time is that of
+// its longest sequence once the others no longer fill the chip, so that one starts
+// first.  Sorted by buckets, four to a doubling (the order inside a bucket is free: it
+// steers the schedule alone).  One workgroup.
+constexpr int PLAN_B = 128;
+__device__ __forceinline__ int plan_bucket(int64_t n) {
+    const unsigned c = (unsigned)((n + 63) / 64);  // 1 .. 2^25
+    const int lg = 31 - __builtin_clz(c);
+    return PLAN_B - 1 - (4 * lg + (int)(((uint64_t)c << 2 >> lg) & 3));
+}
+__device__ __forceinline__ void make_plan(const GdnRaggedArgs &a, int *at, int tid) {
+    if (tid < PLAN_B) at[tid] = 0;
+    __syncthreads();
+    auto length = [&](int i) {
+        const Seq s = seq_of(a.r, i);
+        return s.slot < 0 || s.end - s.begin <= a.longer ? (int64_t)0 : s.end - s.begin;
+    };
+    for (int i = tid; i < a.r.N; i += 256)
+        if (const int64_t n = length(i)) atomicAdd(&at[plan_bucket(n)], 1);
+    __syncthreads();
+    if (tid < 64) {  // counts become first places, two buckets a lane
+        const int c0 = at[2 * tid], c1 = at[2 * tid + 1];
+        int sum = c0 + c1;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const int y = __shfl_up(sum, o, 64);
+            if (tid >= o) sum += y;
+        }
+        at[2 * tid] = sum - c0 - c1;
+        at[2 * tid + 1] = sum - c1;
+        if (tid == 63) a.plan[0] = sum;
+    }
+    __syncthreads();
+    for (int i = tid; i < a.r.N; i += 256)
+        if (const int64_t n = length(i)) a.plan[1 + atomicAdd(&at[plan_bucket(n)], 1)] = i;
+}
+
 // ---------------------------------------------------------------- T and P of a chunk
 template <int DK>
-__global__ void __launch_bounds__(256) k_rag_prep(GdnRaggedArgs a) {
+__global__ void __launch_bounds__(256, 4) k_rag_prep(GdnRaggedArgs a) {
     constexpr int NT = 256, LD = DK + 16, SW = swx<__bf16, DK>(), LA = 68;
-    __shared__ __attribute__((aligned(16))) __bf16 sK[64 * LD], sQ[64 * LD];
-    __shared__ __attribute__((aligned(16))) float sA[64 * LA], sT[64 * LA];
+    // A lies where K's tile was: its products are in registers by then
+    constexpr int KB = 64 * LD * 2 > 64 * LA * 4 ? 64 * LD * 2 : 64 * LA * 4;
+    __shared__ __attribute__((aligned(16))) char mem[KB];
+    __bf16 *const sK = reinterpret_cast<__bf16 *>(mem);
+    float *const sA = reinterpret_cast<float *>(mem);
+    __shared__ __attribute__((aligned(16))) float sT[64 * LA];
     __shared__ __attribute__((aligned(16))) float sb[64], sbeta[64];
     const int tid = threadIdx.x, lane = tid & 63, q4 = lane >> 4, n16 = lane & 15;
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int hk = blockIdx.x % a.Hk, group = a.Hv / a.Hk;
-    const int64_t id = blockIdx.x / a.Hk;
+    if (blockIdx.x == 0) {
+        make_plan(a, reinterpret_cast<int *>(mem), tid);
+        return;
+    }
+    const unsigned block = blockIdx.x - 1;
+    const int hk = block % a.Hk, group = a.Hv / a.Hk;
+    const int64_t id = block / a.Hk;
     const int i = find_seq(a.r, 64, id);
     const Seq sq = seq_of(a.r, i);
     const int64_t c0 = (id - first_run(sq, 64, i)) * 64, n = sq.end - sq.begin;
     if (c0 < 0 || c0 >= n || n <= a.longer || sq.slot < 0) return;
     const int m = n - c0 < 64 ? (int)(n - c0) : 64;
     const int64_t row0 = sq.begin + c0;
+    // rows past the end stand for the last one: beta is 0 there, and their rows of P
+    // make outputs that are not stored
     RowTile<DK, NT, LD, SW> t;
     t.load((const __bf16 *)a.k + row0 * a.sq_t + hk * a.sq_h, a.sq_t, m, tid);
+    bf16x8 qt[DK / 32];
+    {
+        const __bf16 *q = (const __bf16 *)a.q + (row0 + min(16 * w + n16, m - 1)) * a.sq_t + hk * a.sq_h + 8 * q4;
+#pragma unroll
+        for (int ks = 0; ks < DK / 32; ++ks) qt[ks] = *reinterpret_cast<const bf16x8 *>(q + 32 * ks);
+    }
     t.store(sK, tid);
-    t.load((const __bf16 *)a.q + row0 * a.sq_t + hk * a.sq_h, a.sq_t, m, tid);
-    t.store(sQ, tid);
     __syncthreads();
     // wave w: rows 16 w .. of k.k and q.k, columns s in plain pairs
     const LaneOff swo = swz_off<__bf16, LD, SW>(lane);
@@ -146,19 +197,18 @@ __global__ void __launch_bounds__(256) k_rag_prep(GdnRaggedArgs a) {
 #pragma unroll
     for (int ks = 0; ks < DK / 32; ++ks) {
         const bf16x8 kt = ldfrag_swz<__bf16, LD, SW>(sK, swo, 16 * w, 32 * ks);
-        const bf16x8 qt = ldfrag_swz<__bf16, LD, SW>(sQ, swo, 16 * w, 32 * ks);
 #pragma unroll
         for (int st = 0; st < 4; ++st) {
             if (st >= 2 && w < 2) continue;  // above the diagonal
             const bf16x8 kf = *reinterpret_cast<const bf16x8 *>(
                 &sK[(ar + 32 * (st >> 1) + 4 * (st & 1)) * LD + 8 * q4 + 32 * ks + (((32 * ks) & SW) ? -sgn : sgn)]);
             mma(kk[st], kf, kt);
-            mma(qk[st], kf, qt);
+            mma(qk[st], kf, qt[ks]);
         }
     }
     const int tok = 16 * w + n16;
     for (int hv = hk * group; hv < (hk + 1) * group; ++hv) {
-        __syncthreads();  // the last head is done with the gates and with T
+        __syncthreads();  // the last head is done with the gates, with A and T (the first: all with K)
         if (w == 0) {
             const bool in = lane < m;
             const int64_t go = (row0 + lane) * a.sg_t + hv * a.sg_h;
@@ -271,28 +321,29 @@ __global__ void __launch_bounds__(256) k_rag_prep(GdnRaggedArgs a) {
 // into registers a chunk ahead and pass LDS only where K is read transposed.
 // Everything a chunk loads is waited for at one place, before the last chunk's outputs
 // are stored: loads and stores share a counter (see vm_wait_all).
+// LDS of a walk workgroup.  NC >= 2: K's tile and U's pieces lie where S's pieces were,
+// so that two workgroups share a CU; one barrier more keeps the next chunk's S behind
+// their last reads.
 template <int DK, int NC>
-__global__ void __launch_bounds__(256, 2) k_rag_walk(GdnRaggedArgs a) {
+struct WalkLds {
+    static constexpr int LD = DK + 16, CW = 16 * NC, LS = DK + 16, LT = 64 + 16;
+    static constexpr bool ALIAS = NC >= 2;
+    static constexpr int NSP = 3 * CW * LS, NX = 3 * CW * LT, NU = 5 * CW * LT, NKT = 64 * LD;
+    static constexpr int SIZE = NX + (ALIAS ? (NSP > NU + NKT ? NSP : NU + NKT) : NSP + NU + NKT);
+};
+
+// One item: 16 NC columns of one value head of sequence i.
+template <int DK, int NC>
+__device__ __forceinline__ void rag_walk(const GdnRaggedArgs &a, __bf16 *mem, int i, int h, int cb) {
     constexpr int NK = DK / 32, NS = DK / 64;              // k-steps; state tiles of a wave
-    constexpr int LD = DK + 16, SW = swx<__bf16, DK>();    // K tile
-    constexpr int CW = 16 * NC, LS = DK + 16, LT = 64 + 16;  // pieces [column][row], pitches
-    // NC >= 2: K's tile and U's pieces lie where S's pieces were, so that two workgroups
-    // share a CU; one barrier more keeps the next chunk's S behind their last reads
-    constexpr bool ALIAS = NC >= 2;
-    constexpr int NSP = 3 * CW * LS, NX = 3 * CW * LT, NU = 5 * CW * LT, NKT = 64 * LD;
-    __shared__ __attribute__((aligned(16))) __bf16 mem[NX + (ALIAS ? (NSP > NU + NKT ? NSP : NU + NKT) : NSP + NU + NKT)];
-    __bf16 *const sX = mem, *const sS = mem + NX, *const sU = ALIAS ? sS : sS + NSP, *const sK = sU + NU;
+    constexpr int SW = swx<__bf16, DK>(), CW = 16 * NC;    // K tile's swizzle; columns
+    typedef WalkLds<DK, NC> L;
+    constexpr bool ALIAS = L::ALIAS;
+    __bf16 *const sX = mem, *const sS = mem + L::NX, *const sU = ALIAS ? sS : sS + L::NSP, *const sK = sU + L::NU;
     const int tid = threadIdx.x, lane = tid & 63, q4 = lane >> 4, n16 = lane & 15;
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
-    // (sequence, value head) pairs eight at a time, their column blocks eight apart: the
-    // blocks of a pair run on one XCD, whose L2 then holds what they share
-    const int ncb = a.Dv / CW;
-    const int64_t pair = ((int64_t)blockIdx.x / (8 * ncb)) * 8 + blockIdx.x % 8;
-    const int cb = (int)(blockIdx.x / 8 % ncb), h = (int)(pair % a.Hv), i = (int)(pair / a.Hv);
-    if (i >= a.r.N) return;
     const Seq s = seq_of(a.r, i);
     const int64_t n = s.end - s.begin;
-    if (n <= a.longer || s.slot < 0) return;
     const int hk = h / (a.Hv / a.Hk), tok = 16 * w + n16;
     // bases are uniform, a chunk's rows 32-bit offsets from them
     const char *const K = (const char *)a.k + 2 * (s.begin * a.sq_t + hk * a.sq_h);
@@ -378,7 +429,7 @@ __global__ void __launch_bounds__(256, 2) k_rag_walk(GdnRaggedArgs a) {
     fetch_t(sys);
     fetch_p(sys);
     fetch_gates(sys);
-    const LaneOff tr = tr_off<__bf16, LD, SW>(lane);
+    const LaneOff tr = tr_off<__bf16, L::LD, SW>(lane);
     bf16x4 out[NC];
     const char *next = sys;
     for (int64_t c = 0; c < n; c += 64) {
@@ -394,7 +445,7 @@ __global__ void __launch_bounds__(256, 2) k_rag_walk(GdnRaggedArgs a) {
                 split3(S[t][x], f[0], f[1], f[2]);
 #pragma unroll
                 for (int p = 0; p < 3; ++p)
-                    *reinterpret_cast<bf16x4 *>(sS + (p * CW + 16 * x + n16) * LS + 16 * (NS * w + t) + 4 * q4) = f[p];
+                    *reinterpret_cast<bf16x4 *>(sS + (p * CW + 16 * x + n16) * L::LS + 16 * (NS * w + t) + 4 * q4) = f[p];
             }
         vm_wait_all();
         if (c > 0) {
@@ -402,19 +453,33 @@ __global__ void __launch_bounds__(256, 2) k_rag_walk(GdnRaggedArgs a) {
             for (int x = 0; x < NC; ++x) *reinterpret_cast<bf16x4 *>(O + (c - 64) * a.so_t + 16 * x) = out[x];
         }
         __syncthreads();
+        // Operand fragments are read a step ahead of their products, and the fences keep it
+        // so: left alone, the compiler may read each pair just before its use, and then
+        // every two matrix instructions wait for LDS.
         f32x4 X[NC], Y[NC];  // K S (rows: tokens 16 w + 4 q4 + r), (Q S)^T (columns: tokens 16 w + n16)
+        {
+            bf16x8 f[2][NK];
+            auto read = [&](int step) {  // column tile step / 3, piece 2 - step % 3
 #pragma unroll
-        for (int x = 0; x < NC; ++x) X[x] = Y[x] = f32x4{0.f, 0.f, 0.f, 0.f};
+                for (int ks = 0; ks < NK; ++ks)
+                    f[step & 1][ks] = *reinterpret_cast<const bf16x8 *>(
+                        sS + ((2 - step % 3) * CW + 16 * (step / 3) + n16) * L::LS + 32 * ks + 8 * q4);
+            };
+            read(0);
 #pragma unroll
-        for (int x = 0; x < NC; ++x)
-#pragma unroll
-            for (int p = 2; p >= 0; --p)
+            for (int step = 0; step < 3 * NC; ++step) {
+                const int x = step / 3;
+                if (step + 1 < 3 * NC) read(step + 1);
+                sched_fence();
+                if (step % 3 == 0) X[x] = Y[x] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int ks = 0; ks < NK; ++ks) {
-                    const bf16x8 f = *reinterpret_cast<const bf16x8 *>(sS + (p * CW + 16 * x + n16) * LS + 32 * ks + 8 * q4);
-                    mma(X[x], kf[ks], f);
-                    mma(Y[x], f, qf[ks]);
+                    mma(X[x], kf[ks], f[step & 1][ks]);
+                    mma(Y[x], f[step & 1][ks], qf[ks]);
                 }
+                sched_fence();
+            }
+        }
 #pragma unroll
         for (int x = 0; x < NC; ++x) {
 #pragma unroll
@@ -424,14 +489,23 @@ __global__ void __launch_bounds__(256, 2) k_rag_walk(GdnRaggedArgs a) {
             split3(X[x], f[0], f[1], f[2]);
 #pragma unroll
             for (int p = 0; p < 3; ++p)
-                *reinterpret_cast<bf16x4 *>(sX + (p * CW + 16 * x + n16) * LT + 16 * w + 4 * q4) = f[p];
+                *reinterpret_cast<bf16x4 *>(sX + (p * CW + 16 * x + n16) * L::LT + 16 * w + 4 * q4) = f[p];
         }
         if (more) fetch_qv(c + 64);
         __syncthreads();
+        bf16x8 xf[NC][3][2];
+#pragma unroll
+        for (int x = 0; x < NC; ++x)
+#pragma unroll
+            for (int p = 0; p < 3; ++p)
+#pragma unroll
+                for (int ks = 0; ks < 2; ++ks)
+                    xf[x][p][ks] = *reinterpret_cast<const bf16x8 *>(sX + (p * CW + 16 * x + n16) * L::LT + 32 * ks + 8 * q4);
+        sched_fence();
         // K's tile, for the transposed reads (S's pieces have had their last read)
 #pragma unroll
         for (int ks = 0; ks < NK; ++ks)
-            *reinterpret_cast<bf16x8 *>(sK + tok * LD + swz_col(tok, 32 * ks + 8 * q4, SW)) = kf[ks];
+            *reinterpret_cast<bf16x8 *>(sK + tok * L::LD + swz_col(tok, 32 * ks + 8 * q4, SW)) = kf[ks];
         if (more) fetch_k(c + 64);
         f32x4 U[NC];
 #pragma unroll
@@ -442,16 +516,12 @@ __global__ void __launch_bounds__(256, 2) k_rag_walk(GdnRaggedArgs a) {
             for (int ks = 0; ks < 2; ++ks) {
                 if (ks == 1 && !two) continue;
                 const bf16x8(&t)[RAG_TP] = ks ? t1 : t0;
-                bf16x8 f[3];
-#pragma unroll
-                for (int p = 0; p < 3; ++p)
-                    f[p] = *reinterpret_cast<const bf16x8 *>(sX + (p * CW + 16 * x + n16) * LT + 32 * ks + 8 * q4);
-                mma(U1, t[2], f[0]);
-                mma(U[x], t[1], f[1]);
-                mma(U1, t[0], f[2]);
-                mma(U[x], t[1], f[0]);
-                mma(U1, t[0], f[1]);
-                mma(U[x], t[0], f[0]);
+                mma(U1, t[2], xf[x][0][ks]);
+                mma(U[x], t[1], xf[x][1][ks]);
+                mma(U1, t[0], xf[x][2][ks]);
+                mma(U[x], t[1], xf[x][0][ks]);
+                mma(U1, t[0], xf[x][1][ks]);
+                mma(U[x], t[0], xf[x][0][ks]);
             }
             U[x] += U1;
             bf16x4 f[5];
@@ -464,47 +534,68 @@ __global__ void __launch_bounds__(256, 2) k_rag_walk(GdnRaggedArgs a) {
             }
 #pragma unroll
             for (int p = 0; p < 5; ++p)
-                *reinterpret_cast<bf16x4 *>(sU + (p * CW + 16 * x + n16) * LT + 16 * w + 4 * q4) = f[p];
+                *reinterpret_cast<bf16x4 *>(sU + (p * CW + 16 * x + n16) * L::LT + 16 * w + 4 * q4) = f[p];
         }
         if (more) fetch_t(next);
         __syncthreads();
+        auto u_piece = [&](int x, int p, int ks) {
+            return *reinterpret_cast<const bf16x8 *>(sU + (p * CW + 16 * x + n16) * L::LT + 32 * ks + 8 * q4);
+        };
+        bf16x8 po[2][2][2], uf[2][3][2], kt[NS][2];  // U's pair, its pieces, K^T
+        auto read_pair = [&](int x) {
+#pragma unroll
+            for (int p = 0; p < 2; ++p)
+#pragma unroll
+                for (int ks = 0; ks < 2; ++ks) po[x & 1][p][ks] = u_piece(x, 3 + p, ks);
+        };
+        auto read_pieces = [&](int x) {
+#pragma unroll
+            for (int p = 0; p < 3; ++p)
+#pragma unroll
+                for (int ks = 0; ks < 2; ++ks) uf[x & 1][p][ks] = u_piece(x, p, ks);
+        };
+        read_pair(0);
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+            for (int t = 0; t < NS; ++t) kt[t][ks] = ldfragTR<__bf16, L::LD, SW>(sK, tr, 32 * ks, 16 * (NS * w + t));
         // O^T = e^b (Q S)^T + U^T P^T
 #pragma unroll
         for (int x = 0; x < NC; ++x) {
+            if (x + 1 < NC) read_pair(x + 1);
+            else read_pieces(0);
+            sched_fence();
             Y[x] *= et;
 #pragma unroll
             for (int ks = 0; ks < 2; ++ks) {
                 if (ks == 1 && !two) continue;
-                const bf16x8 uh = *reinterpret_cast<const bf16x8 *>(sU + (3 * CW + 16 * x + n16) * LT + 32 * ks + 8 * q4);
-                const bf16x8 ul = *reinterpret_cast<const bf16x8 *>(sU + (4 * CW + 16 * x + n16) * LT + 32 * ks + 8 * q4);
-                mma(Y[x], uh, ks ? p1[1] : p0[1]);
-                mma(Y[x], ul, ks ? p1[0] : p0[0]);
-                mma(Y[x], uh, ks ? p1[0] : p0[0]);
+                mma(Y[x], po[x & 1][0][ks], ks ? p1[1] : p0[1]);
+                mma(Y[x], po[x & 1][1][ks], ks ? p1[0] : p0[0]);
+                mma(Y[x], po[x & 1][0][ks], ks ? p1[0] : p0[0]);
             }
-#pragma unroll
-            for (int r = 0; r < 4; ++r) out[x][r] = (__bf16)Y[x][r];
+            sched_fence();
         }
         if (more) fetch_p(next);
         // S = e^(b_63) S + K^T e^(b_63 - b) U
 #pragma unroll
-        for (int t = 0; t < NS; ++t)
+        for (int x = 0; x < NC; ++x) {
+            if (x + 1 < NC) read_pieces(x + 1);
+            sched_fence();
 #pragma unroll
-            for (int x = 0; x < NC; ++x) S[t][x] *= gam;
-        if (more) fetch_gates(next);
+            for (int t = 0; t < NS; ++t) S[t][x] *= gam;
+            if (x + 1 == NC && more) fetch_gates(next);
 #pragma unroll
-        for (int ks = 0; ks < 2; ++ks) {
-            bf16x8 kt[NS];
+            for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
-            for (int t = 0; t < NS; ++t) kt[t] = ldfragTR<__bf16, LD, SW>(sK, tr, 32 * ks, 16 * (NS * w + t));
+                for (int p = 2; p >= 0; --p)
 #pragma unroll
-            for (int x = 0; x < NC; ++x)
-#pragma unroll
-                for (int p = 2; p >= 0; --p) {
-                    const bf16x8 f = *reinterpret_cast<const bf16x8 *>(sU + (p * CW + 16 * x + n16) * LT + 32 * ks + 8 * q4);
-#pragma unroll
-                    for (int t = 0; t < NS; ++t) mma(S[t][x], kt[t], f);
-                }
+                    for (int t = 0; t < NS; ++t) mma(S[t][x], kt[t][ks], uf[x & 1][p][ks]);
+            sched_fence();
         }
+#pragma unroll
+        for (int x = 0; x < NC; ++x)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) out[x][r] = (__bf16)Y[x][r];
     }
     const int64_t last = (n - 1) / 64 * 64;
     if (last + tok < n) {
@@ -519,24 +610,54 @@ __global__ void __launch_bounds__(256, 2) k_rag_walk(GdnRaggedArgs a) {
             for (int r = 0; r < 4; ++r) st[(int64_t)(16 * t + r) * a.Dv + 16 * x] = S[t][x][r];
 }
 
+// Items of the walk over the planned sequences, in steps of `groups` workgroups: pairs of
+// a sequence and a value head eight at a time, their column blocks eight apart, so that
+// the blocks of a pair run on one XCD, whose L2 then holds what they share.
+template <int DK, int NC>
+__device__ __forceinline__ void rag_walk_items(const GdnRaggedArgs &a, __bf16 *mem, int count, int groups) {
+    const int ncb = a.Dv / (16 * NC);
+    const int64_t items = gdn_walk_items(a, count, NC);
+    for (int64_t id = blockIdx.x; id < items; id += groups) {
+        const int64_t pair = id / (8 * ncb) * 8 + id % 8;
+        const int rank = (int)(pair / a.Hv);
+        if (rank >= count) continue;
+        if (id >= groups) __syncthreads();  // the last item is done with the LDS
+        rag_walk<DK, NC>(a, mem, __builtin_amdgcn_readfirstlane(a.plan[1 + rank]), (int)(pair % a.Hv), (int)(id / 8 % ncb));
+    }
+}
+
+// The long sequences' walk, and beside it, behind its workgroups, the tokens of the
+// short ones: the walk waits for its own chain, the tokens for memory.
+template <int DK>
+__global__ void __launch_bounds__(256, 2) k_rag_walk(GdnRaggedArgs a, int groups) {
+    constexpr int S1 = WalkLds<DK, 1>::SIZE, S2 = WalkLds<DK, 2>::SIZE;
+    __shared__ __attribute__((aligned(16))) __bf16 mem[S1 > S2 ? S1 : S2];
+    if ((int)blockIdx.x >= groups) {
+        gdn_tokens<__bf16, DK, TOK_CL>(a, (int64_t)(blockIdx.x - groups) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6));
+        return;
+    }
+    // two column tiles an item share what a chunk loads; one alone is faster where every
+    // item has a CU to itself (4096 tokens: 20 heads,
+    // 160 items of one tile, 143 us against 192; three times as many 255 against 222)
+    const int count = __builtin_amdgcn_readfirstlane(a.plan[0]);
+    if (gdn_walk_items(a, count, 1) <= a.n_cu) rag_walk_items<DK, 1>(a, mem, count, groups);
+    else rag_walk_items<DK, 2>(a, mem, count, groups);
+}
+
 }  // namespace
 
 hipError_t launch_gdn_chunk_prep(const GdnRaggedArgs &a, hipStream_t s, hipEvent_t e0, hipEvent_t e1) {
-    const dim3 grid((unsigned)(a.n_chunks * a.Hk));
+    const dim3 grid((unsigned)(a.n_chunks * a.Hk + 1));
     if (a.Dk == 128) hipExtLaunchKernelGGL((k_rag_prep<128>), grid, dim3(256), 0, s, e0, e1, 0, a);
     else hipExtLaunchKernelGGL((k_rag_prep<64>), grid, dim3(256), 0, s, e0, e1, 0, a);
     return hipGetLastError();
 }
 
 hipError_t launch_gdn_chunk_walk(const GdnRaggedArgs &a, hipStream_t s, hipEvent_t e0, hipEvent_t e1) {
-    auto go = [&](auto nc) {
-        constexpr int NC = decltype(nc)::value;
-        const dim3 grid((unsigned)gdn_walk_groups(a, NC)), block(256);
-        if (a.Dk == 128) hipExtLaunchKernelGGL((k_rag_walk<128, NC>), grid, block, 0, s, e0, e1, 0, a);
-        else hipExtLaunchKernelGGL((k_rag_walk<64, NC>), grid, block, 0, s, e0, e1, 0, a);
-    };
-    if (gdn_walk_tiles(a) == 1) go(std::integral_constant<int, 1>());
-    else go(std::integral_constant<int, 2>());
+    const int groups = (int)gdn_walk_groups(a);
+    const dim3 grid((unsigned)(groups + (gdn_token_waves(a) + 3) / 4)), block(256);
+    if (a.Dk == 128) hipExtLaunchKernelGGL((k_rag_walk<128>), grid, block, 0, s, e0, e1, 0, a, groups);
+    else hipExtLaunchKernelGGL((k_rag_walk<64>), grid, block, 0, s, e0, e1, 0, a, groups);
     return hipGetLastError();
 }
 

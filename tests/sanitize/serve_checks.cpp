@@ -199,14 +199,16 @@ int main() {
     REFUSED(Gdn, run, SF_OK, )
     REFUSED(Gdn, run, SF_OK, c.s.sq_t = c.s.sq_h = c.s.sv_t = c.s.sv_h = c.s.sg_t = c.s.sg_h = 0)  // broadcast inputs
     REFUSED(Gdn, run, SF_OK, c.b.n_slots = 1; c.s.ss = 0)
-    EXPECT(rec.gdn.size() == 3 && rec.gdn[0].Hv == 8 && rec.gdn[0].r.N == 3 && rec.gdn[1].sq_t == 0);
-    EXPECT(sf::gdn_token_waves(rec.gdn[0]) == 3 * 8 * 4);
-    // long sequences: a system of every chunk and head in the workspace
-    EXPECT(rec.prep.size() == 3 && rec.walk.size() == 3 && rec.prep[0].n_chunks == 100 / 64 + 3);
+    // a long sequence: the systems and the plan, then the walk with the other tokens
+    EXPECT(rec.gdn.empty() && rec.prep.size() == 3 && rec.walk.size() == 3);
+    EXPECT(rec.walk[0].Hv == 8 && rec.walk[0].r.N == 3 && rec.walk[1].sq_t == 0);
+    EXPECT(rec.walk[0].n_chunks == 100 / 64 + 3 && rec.walk[0].longer == sf::RAG_LONG);
+    EXPECT(sf::gdn_token_waves(rec.walk[0]) == 3 * 8 * 4);
     {
         Gdn c;
         const size_t need = sf_gdn_ragged_workspace_bytes(&c.s, &c.b);
-        EXPECT(need == (size_t)4 * 8 * sf::RAG_SYS);
+        EXPECT(need == (size_t)4 * 8 * sf::RAG_SYS + 4 * 4);
+        EXPECT((char *)rec.walk[0].plan == rec.walk[0].ws + 4 * 8 * sf::RAG_SYS);
         c.ws_bytes = need;
         EXPECT(c.run() == SF_OK);
         c.ws_bytes = need - 1;
@@ -221,8 +223,21 @@ int main() {
         EXPECT(sf_gdn_ragged_workspace_bytes(&c.s, &c.b) == 0 && c.run() == SF_OK);
         c.b.max_len = 90, c.s.io_dtype = SF_F32;
         EXPECT(sf_gdn_ragged_workspace_bytes(&c.s, &c.b) == 0 && c.run() == SF_OK);
-        EXPECT(rec.prep.size() == 4 && rec.gdn.size() == 6 && rec.gdn[5].longer == 0);
+        c.s.io_dtype = SF_BF16, c.s.sq_t = 1 << 23;  // 64 rows of 1 GiB: token by token
+        EXPECT(sf_gdn_ragged_workspace_bytes(&c.s, &c.b) == 0 && c.run() == SF_OK);
+        EXPECT(rec.prep.size() == 4 && rec.gdn.size() == 3 && rec.gdn[2].longer == 0);
     }
+    // every item has a workgroup or follows one, whatever the sizes; columns cover Dv
+    for (int N : {1, 7, 3000})
+        for (int Hv : {1, 3, 40})
+            for (int Dv : {64, 128, 256})
+                for (int nc : {1, 2}) {
+                    sf::GdnRaggedArgs a = rec.walk[0];
+                    a.r.N = N, a.Hv = Hv, a.Dv = Dv;
+                    const int64_t items = sf::gdn_walk_items(a, N, nc), groups = sf::gdn_walk_groups(a);
+                    EXPECT(groups % 8 == 0 && groups >= 8 && (groups >= items || groups == 8 * a.n_cu));
+                    EXPECT(items % (8 * (Dv / (16 * nc))) == 0 && items >= (int64_t)N * Hv * (Dv / (16 * nc)));
+                }
     // chunk numbers stay below n_chunks whatever the bounds, decreasing ones too
     for (int b = 0; b <= 200; ++b)
         for (int e = b + 1; e <= 200; ++e) EXPECT(b / 64 + 4 + (e - b + 63) / 64 <= 200 / 64 + 5);

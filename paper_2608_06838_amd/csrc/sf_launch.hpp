@@ -152,7 +152,7 @@ struct GdnRaggedArgs {
     int32_t longer;    // sequences of more tokens are taken in chunks (0: none are)
     int64_t n_chunks;  // upper bound of the chunks: T / 64 + N
     char *ws;          // chunk systems: [n_chunks][Hv] of RAG_SYS bytes
-    int32_t *plan;     // [1 + N], see gdn_plan_at
+    int32_t *plan;     // [2 + N], see gdn_plan_at
 };
 // waves of the token-by-token kernel: one for each sequence, value head and tile of 4 TOK_CL columns
 constexpr int TOK_CL = 8;
@@ -172,10 +172,10 @@ inline int64_t gdn_walk_groups(const GdnRaggedArgs &a) {
     const int64_t n = gdn_walk_items(a, a.r.N, 1), most = 8 * (int64_t)a.n_cu;
     return n < most ? n : most;
 }
-// behind the chunk systems: how many sequences are taken in chunks, then their numbers,
-// longest first
+// behind the chunk systems: how many sequences are taken in chunks, how many of them in
+// single column tiles, then their numbers, longest first
 inline size_t gdn_plan_at(const GdnRaggedArgs &a) { return (size_t)a.n_chunks * (size_t)a.Hv * RAG_SYS; }
-inline size_t gdn_chunk_ws_bytes(const GdnRaggedArgs &a) { return gdn_plan_at(a) + 4 * ((size_t)a.r.N + 1); }
+inline size_t gdn_chunk_ws_bytes(const GdnRaggedArgs &a) { return gdn_plan_at(a) + 4 * ((size_t)a.r.N + 2); }
 // T and P of every chunk and the plan; then the walk, with the other sequences' tokens
 hipError_t launch_gdn_chunk_prep(const GdnRaggedArgs &a, hipStream_t s, hipEvent_t e0, hipEvent_t e1);
 hipError_t launch_gdn_chunk_walk(const GdnRaggedArgs &a, hipStream_t s, hipEvent_t e0, hipEvent_t e1);

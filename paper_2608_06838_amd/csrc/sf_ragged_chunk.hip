@@ -116,38 +116,57 @@ __device__ __forceinline__ constexpr int tri_frag(int tt, int ks) { return tt < 
 // The sequences that are taken in chunks, longest first: the walk's time is that of
 // its longest sequence once the others no longer fill the chip, so that one starts
 // first.  Sorted by buckets, four to a doubling (the order inside a bucket is free: it
-// steers the schedule alone).  One workgroup.
+// steers the schedule alone).  A sequence with more chunks than a CU's share of all
+// chunk steps is what the launch waits for: it is walked in single column tiles, whose
+// step is shorter, as long as each has a CU of its own; the others in pairs of tiles,
+// which share what a chunk loads.  (Chunk steps, us: alone on a CU 2.2 single, 3.4 in
+// pairs; with the CUs full 1.9 a single tile, 2.8 a pair.)  One workgroup.
 constexpr int PLAN_B = 128;
 __device__ __forceinline__ int plan_bucket(int64_t n) {
     const unsigned c = (unsigned)((n + 63) / 64);  // 1 .. 2^25
     const int lg = 31 - __builtin_clz(c);
     return PLAN_B - 1 - (4 * lg + (int)(((uint64_t)c << 2 >> lg) & 3));
 }
+// the fewest chunks of a bucket
+__device__ __forceinline__ int64_t bucket_chunks(int b) {
+    const int e = PLAN_B - 1 - b, lg = e >> 2;
+    return (((int64_t)(4 + (e & 3)) << lg) + 3) >> 2;
+}
 __device__ __forceinline__ void make_plan(const GdnRaggedArgs &a, int *at, int tid) {
-    if (tid < PLAN_B) at[tid] = 0;
+    int *const sum = at + PLAN_B, *const single = sum + 1;
+    if (tid < PLAN_B + 2) at[tid] = 0;
     __syncthreads();
     auto length = [&](int i) {
         const Seq s = seq_of(a.r, i);
         return s.slot < 0 || s.end - s.begin <= a.longer ? (int64_t)0 : s.end - s.begin;
     };
     for (int i = tid; i < a.r.N; i += 256)
-        if (const int64_t n = length(i)) atomicAdd(&at[plan_bucket(n)], 1);
+        if (const int64_t n = length(i)) {
+            atomicAdd(&at[plan_bucket(n)], 1);
+            atomicAdd(sum, (int)((n + 63) / 64));
+        }
     __syncthreads();
     if (tid < 64) {  // counts become first places, two buckets a lane
         const int c0 = at[2 * tid], c1 = at[2 * tid + 1];
-        int sum = c0 + c1;
+        int first = c0 + c1;
 #pragma unroll
         for (int o = 1; o < 64; o <<= 1) {
-            const int y = __shfl_up(sum, o, 64);
-            if (tid >= o) sum += y;
+            const int y = __shfl_up(first, o, 64);
+            if (tid >= o) first += y;
         }
-        at[2 * tid] = sum - c0 - c1;
-        at[2 * tid + 1] = sum - c1;
-        if (tid == 63) a.plan[0] = sum;
+        const int64_t share = (int64_t)*sum * a.Hv * (a.Dv / 32) / a.n_cu, most = a.n_cu / (a.Hv * (a.Dv / 16));
+        int own = 0;  // sequences of this lane's buckets that get single tiles
+        if (bucket_chunks(2 * tid) > share && first - c1 <= most) own = c0;
+        if (bucket_chunks(2 * tid + 1) > share && first <= most) own += c1;
+        if (own) atomicAdd(single, own);
+        at[2 * tid] = first - c0 - c1;
+        at[2 * tid + 1] = first - c1;
+        if (tid == 63) a.plan[0] = first;
     }
     __syncthreads();
+    if (tid == 0) a.plan[1] = *single;
     for (int i = tid; i < a.r.N; i += 256)
-        if (const int64_t n = length(i)) a.plan[1 + atomicAdd(&at[plan_bucket(n)], 1)] = i;
+        if (const int64_t n = length(i)) a.plan[2 + atomicAdd(&at[plan_bucket(n)], 1)] = i;
 }
 
 // ---------------------------------------------------------------- T and P of a chunk
@@ -610,19 +629,23 @@ __device__ __forceinline__ void rag_walk(const GdnRaggedArgs &a, __bf16 *mem, in
             for (int r = 0; r < 4; ++r) st[(int64_t)(16 * t + r) * a.Dv + 16 * x] = S[t][x][r];
 }
 
-// Items of the walk over the planned sequences, in steps of `groups` workgroups: pairs of
-// a sequence and a value head eight at a time, their column blocks eight apart, so that
-// the blocks of a pair run on one XCD, whose L2 then holds what they share.
+// Items of the walk over the planned sequences from..to, numbered from `first` on, in
+// steps of the launch's workgroups: pairs of a sequence and a value head eight at a time,
+// their column blocks eight apart, so that the blocks of a pair run on one XCD, whose L2
+// then holds what they share.
 template <int DK, int NC>
-__device__ __forceinline__ void rag_walk_items(const GdnRaggedArgs &a, __bf16 *mem, int count, int groups) {
+__device__ __forceinline__ void rag_walk_items(const GdnRaggedArgs &a, __bf16 *mem, int from, int to, int64_t first,
+                                               int groups) {
     const int ncb = a.Dv / (16 * NC);
-    const int64_t items = gdn_walk_items(a, count, NC);
-    for (int64_t id = blockIdx.x; id < items; id += groups) {
+    const int64_t items = gdn_walk_items(a, to - from, NC);
+    int64_t id = (int64_t)blockIdx.x - first % groups;
+    if (id < 0) id += groups;
+    for (; id < items; id += groups) {
         const int64_t pair = id / (8 * ncb) * 8 + id % 8;
-        const int rank = (int)(pair / a.Hv);
-        if (rank >= count) continue;
-        if (id >= groups) __syncthreads();  // the last item is done with the LDS
-        rag_walk<DK, NC>(a, mem, __builtin_amdgcn_readfirstlane(a.plan[1 + rank]), (int)(pair % a.Hv), (int)(id / 8 % ncb));
+        const int rank = from + (int)(pair / a.Hv);
+        if (rank >= to) continue;
+        __syncthreads();  // the last item is done with the LDS
+        rag_walk<DK, NC>(a, mem, __builtin_amdgcn_readfirstlane(a.plan[2 + rank]), (int)(pair % a.Hv), (int)(id / 8 % ncb));
     }
 }
 
@@ -636,12 +659,9 @@ __global__ void __launch_bounds__(256, 2) k_rag_walk(GdnRaggedArgs a, int groups
         gdn_tokens<__bf16, DK, TOK_CL>(a, (int64_t)(blockIdx.x - groups) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6));
         return;
     }
-    // two column tiles an item share what a chunk loads; one alone is faster where every
-    // item has a CU to itself (4096 tokens: 20 heads,
-    // 160 items of one tile, 143 us against 192; three times as many 255 against 222)
-    const int count = __builtin_amdgcn_readfirstlane(a.plan[0]);
-    if (gdn_walk_items(a, count, 1) <= a.n_cu) rag_walk_items<DK, 1>(a, mem, count, groups);
-    else rag_walk_items<DK, 2>(a, mem, count, groups);
+    const int count = __builtin_amdgcn_readfirstlane(a.plan[0]), single = __builtin_amdgcn_readfirstlane(a.plan[1]);
+    rag_walk_items<DK, 1>(a, mem, 0, single, 0, groups);
+    rag_walk_items<DK, 2>(a, mem, single, count, gdn_walk_items(a, single, 1), groups);
 }
 
 }  // namespace

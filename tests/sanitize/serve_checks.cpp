@@ -207,7 +207,7 @@ int main() {
     {
         Gdn c;
         const size_t need = sf_gdn_ragged_workspace_bytes(&c.s, &c.b);
-        EXPECT(need == (size_t)4 * 8 * sf::RAG_SYS + 4 * 4);
+        EXPECT(need == (size_t)4 * 8 * sf::RAG_SYS + 4 * 5);
         EXPECT((char *)rec.walk[0].plan == rec.walk[0].ws + 4 * 8 * sf::RAG_SYS);
         c.ws_bytes = need;
         EXPECT(c.run() == SF_OK);

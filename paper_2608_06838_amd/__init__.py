@@ -32,6 +32,7 @@ Norms of queries and keys for each head, with the position rotation in the same 
     q', k'                   = qk_norm_fwd(q, k, norm="l2")
     dq, dk, dwq, dwk         = qk_norm_bwd(q, k, dq', dk', norm="l2")
 """
+import contextlib
 import ctypes
 
 import torch
@@ -583,12 +584,37 @@ def partition_hybrid(T, N, alpha, w_tok, w_soft, round_to=128):
     return [int(x) for x in out]
 
 
-def _on_gpu(ref, **ts):
+# The serving calls run for every token, where the time of a call is the host's: they
+# marshal by position, hand over plain integers and enter a stream only where it is not
+# the current one already.
+
+def _on_gpu(ref, *ts):
     """The library works on device memory of one GPU: a host tensor, or one of another
     GPU, would reach a kernel as a bad address."""
-    for name, t in ts.items():
-        if t is not None and (not t.is_cuda or t.device != ref.device):
-            raise ValueError(f"{name} must be on {ref.device if ref.is_cuda else 'the GPU'}, it is on {t.device}")
+    dev = ref.get_device()
+    for t in ts:
+        if t is not None and (t.get_device() != dev or dev < 0):
+            raise ValueError(f"all tensors must be on one GPU, got {ref.device} and {t.device}")
+    if dev < 0:
+        raise ValueError(f"all tensors must be on one GPU, got {ref.device}")
+    return dev
+
+
+def _on(dev, stream):
+    """(context in which the call's tensors are allocated and its kernels launched, the
+    stream's handle)."""
+    if stream is not None:
+        return torch.cuda.stream(stream), stream.cuda_stream
+    ctx = contextlib.nullcontext() if torch.cuda.current_device() == dev else torch.cuda.device(dev)
+    return ctx, torch.cuda.current_stream(dev).cuda_stream
+
+
+def _addr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _timed(timing):
+    return None if timing is None else ctypes.byref(_tuning(timing=timing))
 
 
 def _ragged(T, state, cu_seqlens, slots, fresh, max_len):
@@ -601,11 +627,9 @@ def _ragged(T, state, cu_seqlens, slots, fresh, max_len):
     if fresh is not None and (tuple(fresh.shape) != (N,) or fresh.dtype not in (torch.uint8, torch.bool)
                               or not fresh.is_contiguous()):
         raise ValueError(f"fresh must be a contiguous uint8 or bool tensor of {N} entries")
-    b = _lib.SfRagged()
-    b.N, b.n_slots, b.T = N, N if state is None else state.shape[0], T
-    b.max_len = max(T - N + 1, 1) if max_len is None else int(max_len)
-    b.cu, b.slot, b.fresh = (None if t is None else t.data_ptr() for t in (cu_seqlens, slots, fresh))
-    return b
+    return _lib.SfRagged(N, N if state is None else state.shape[0], T,
+                         max(T - N + 1, 1) if max_len is None else int(max_len), cu_seqlens.data_ptr(), _addr(slots),
+                         _addr(fresh))
 
 
 def _gdn_ragged_args(q, k, v, g, beta, state, cu_seqlens, slots, fresh, max_len, o):
@@ -613,33 +637,32 @@ def _gdn_ragged_args(q, k, v, g, beta, state, cu_seqlens, slots, fresh, max_len,
         raise ValueError("q, k must be [T, Hk, Dk] and v [T, Hv, Dv]")
     if q.dtype not in _IO:
         raise TypeError(f"unsupported I/O dtype {q.dtype}")
-    (T, Hk, Dk), (_, Hv, Dv) = q.shape, v.shape
-    if k.shape != q.shape or k.stride() != q.stride() or k.dtype != q.dtype:
+    (T, Hk, Dk), (Tv, Hv, Dv) = q.shape, v.shape
+    qs, vs, gs, ss = q.stride(), v.stride(), g.stride(), state.stride()
+    if k.shape != q.shape or k.stride() != qs or k.dtype != q.dtype:
         raise ValueError("q and k must share shape, strides and dtype")
-    if v.shape[0] != T or v.dtype != q.dtype:
+    if Tv != T or v.dtype != q.dtype:
         raise ValueError("v must have the tokens and the dtype of q")
-    if q.stride(2) != 1 or v.stride(2) != 1:
+    if qs[2] != 1 or vs[2] != 1:
         raise ValueError("the channel dim must be contiguous")
     for name, t in (("g", g), ("beta", beta)):
-        if tuple(t.shape) != (T, Hv) or t.dtype != torch.float32 or t.stride() != g.stride():
+        if t.shape != (T, Hv) or t.dtype != torch.float32 or t.stride() != gs:
             raise ValueError(f"{name} must be float32 [{T}, {Hv}], with the strides of g")
-    if state.dim() != 4 or tuple(state.shape[1:]) != (Hv, Dk, Dv) or state.dtype != torch.float32 \
-            or (state.numel() and not state[0].is_contiguous()):
+    if state.dim() != 4 or state.shape[1:] != (Hv, Dk, Dv) or state.dtype != torch.float32 \
+            or (state.numel() and ss[1:] != (Dk * Dv, Dv, 1) and not state[0].is_contiguous()):
         raise ValueError(f"state must be float32 [slots, {Hv}, {Dk}, {Dv}], contiguous within a slot")
     if o is not None and (tuple(o.shape) != (T, Hv, Dv) or o.dtype != q.dtype or o.stride(2) != 1):
         raise ValueError("out must match v in shape and dtype, its channels contiguous")
-    _on_gpu(q, q=q, k=k, v=v, g=g, beta=beta, state=state, cu_seqlens=cu_seqlens, slots=slots, fresh=fresh, out=o)
-    sh = _lib.SfGdnRaggedShape()
-    sh.Hk, sh.Hv, sh.Dk, sh.Dv, sh.io_dtype = Hk, Hv, Dk, Dv, _IO[q.dtype]
-    sh.sq_t, sh.sq_h, sh.sv_t, sh.sv_h = q.stride(0), q.stride(1), v.stride(0), v.stride(1)
-    sh.so_t, sh.so_h = (Hv * Dv, Dv) if o is None else o.stride()[:2]
-    sh.sg_t, sh.sg_h, sh.ss = g.stride(0), g.stride(1), state.stride(0)
-    return sh, _ragged(T, state, cu_seqlens, slots, fresh, max_len)
+    dev = _on_gpu(q, k, v, g, beta, state, cu_seqlens, slots, fresh, o)
+    so_t, so_h = (Hv * Dv, Dv) if o is None else o.stride()[:2]
+    sh = _lib.SfGdnRaggedShape(Hk, Hv, Dk, Dv, _IO[q.dtype], 0, qs[0], qs[1], vs[0], vs[1], so_t, so_h, gs[0], gs[1],
+                               ss[0])
+    return dev, sh, _ragged(T, state, cu_seqlens, slots, fresh, max_len)
 
 
 def gdn_ragged_workspace_bytes(q, k, v, g, beta, state, cu_seqlens, slots=None, *, max_len=None):
     """Bytes of the workspace that gdn_ragged_fwd takes as out[1]."""
-    sh, b = _gdn_ragged_args(q, k, v, g, beta, state, cu_seqlens, slots, None, max_len, None)
+    _, sh, b = _gdn_ragged_args(q, k, v, g, beta, state, cu_seqlens, slots, None, max_len, None)
     return _lib.lib().sf_gdn_ragged_workspace_bytes(ctypes.byref(sh), ctypes.byref(b))
 
 
@@ -658,16 +681,20 @@ def gdn_ragged_fwd(q, k, v, g, beta, state, cu_seqlens, slots=None, *, fresh=Non
     max_len: the longest sequence if the host knows it (None: taken for N - 1 sequences
     of one token and one with the rest); it steers the launch, not the result."""
     o, ws = (None, None) if out is None else out
-    sh, b = _gdn_ragged_args(q, k, v, g, beta, state, cu_seqlens, slots, fresh, max_len, o)
-    stream = stream or torch.cuda.current_stream(q.device)
+    dev, sh, b = _gdn_ragged_args(q, k, v, g, beta, state, cu_seqlens, slots, fresh, max_len, o)
+    if ws is not None:
+        _on_gpu(q, ws)
     L_ = _lib.lib()
-    with torch.cuda.stream(stream):
+    ctx, handle = _on(dev, stream)
+    with ctx:
+        nbytes = 0 if ws is None else ws.numel() * ws.element_size()
         if out is None:
             o = torch.empty(v.shape, dtype=v.dtype, device=v.device)
-            ws = _ws(L_.sf_gdn_ragged_workspace_bytes(ctypes.byref(sh), ctypes.byref(b)), q.device)
-        rc = L_.sf_gdn_ragged_fwd(ctypes.byref(sh), ctypes.byref(b), _ptr(q), _ptr(k), _ptr(v), _ptr(g), _ptr(beta),
-                                  _ptr(state), _ptr(o), _ptr(ws), 0 if ws is None else ws.numel() * ws.element_size(),
-                                  ctypes.byref(_tuning(timing=timing)), _stream_handle(stream))
+            nbytes = L_.sf_gdn_ragged_workspace_bytes(ctypes.byref(sh), ctypes.byref(b))
+            ws = _ws(nbytes, v.device) if nbytes else None
+        rc = L_.sf_gdn_ragged_fwd(ctypes.byref(sh), ctypes.byref(b), q.data_ptr(), k.data_ptr(), v.data_ptr(),
+                                  g.data_ptr(), beta.data_ptr(), state.data_ptr(), o.data_ptr(), _addr(ws), nbytes,
+                                  _timed(timing), handle)
     _lib.check("sf_gdn_ragged_fwd", rc)
     return o
 
@@ -689,25 +716,24 @@ def conv_ragged_fwd(x, w, tails, cu_seqlens, slots=None, *, fresh=None, act="sil
     W = w.shape[1]
     if W == 1:
         tails = None
-    elif tails is None or tails.dim() != 3 or tuple(tails.shape[1:]) != (W - 1, C) or tails.dtype != torch.float32 \
-            or (tails.numel() and not tails[0].is_contiguous()):
+    elif tails is None or tails.dim() != 3 or tails.shape[1:] != (W - 1, C) or tails.dtype != torch.float32 \
+            or (tails.numel() and tails.stride()[1:] != (C, 1) and not tails[0].is_contiguous()):
         raise ValueError(f"tails must be float32 [slots, {W - 1}, {C}], contiguous within a slot")
     if out is not None and (out.shape != x.shape or out.dtype != x.dtype or out.stride(1) != 1):
         raise ValueError("out must match x in shape and dtype, its channels contiguous")
     if act not in _ACT:
         raise ValueError(f"act must be one of {sorted(_ACT)}, got {act!r}")
-    _on_gpu(x, x=x, w=w, tails=tails, cu_seqlens=cu_seqlens, slots=slots, fresh=fresh, out=out)
+    dev = _on_gpu(x, w, tails, cu_seqlens, slots, fresh, out)
     b = _ragged(T, tails, cu_seqlens, slots, fresh, max_len)
     if W == 1 and slots is not None:
         b.n_slots = 2 ** 31 - 1  # no tails: only negative slots are out of range
-    sh = _lib.SfConvRaggedShape()
-    sh.C, sh.W, sh.io_dtype, sh.act = C, W, _IO[x.dtype], _ACT[act]
-    sh.sx_t, sh.sy_t, sh.ss = x.stride(0), C if out is None else out.stride(0), 0 if tails is None else tails.stride(0)
-    stream = stream or torch.cuda.current_stream(x.device)
-    with torch.cuda.stream(stream):
+    sh = _lib.SfConvRaggedShape(C, W, _IO[x.dtype], _ACT[act], 0, x.stride(0), C if out is None else out.stride(0),
+                                0 if tails is None else tails.stride(0))
+    ctx, handle = _on(dev, stream)
+    with ctx:
         y = torch.empty((T, C), dtype=x.dtype, device=x.device) if out is None else out
-        rc = _lib.lib().sf_conv_ragged_fwd(ctypes.byref(sh), ctypes.byref(b), _ptr(x), _ptr(w), _ptr(tails), _ptr(y),
-                                           ctypes.byref(_tuning(timing=timing)), _stream_handle(stream))
+        rc = _lib.lib().sf_conv_ragged_fwd(ctypes.byref(sh), ctypes.byref(b), x.data_ptr(), w.data_ptr(),
+                                           _addr(tails), y.data_ptr(), _timed(timing), handle)
     _lib.check("sf_conv_ragged_fwd", rc)
     return y
 
@@ -716,8 +742,8 @@ _NORM = {"none": _lib.SF_NORM_NONE, "l2": _lib.SF_NORM_L2, "rms": _lib.SF_NORM_R
 
 
 def _qk_args(q, k, norm, q_weight, k_weight, eps, q_scale, inv_freq, pos, pos0, interleaved, ys, ds):
-    """The call's shape; ys: outputs or their gradients, ds: the inputs' gradients
-    (None: packed)."""
+    """(device, shape of the call, pos); ys: outputs or their gradients, ds: the inputs'
+    gradients (None: packed)."""
     if q.dim() != 4 or k.dim() != 4 or q.shape[:2] != k.shape[:2] or q.shape[3] != k.shape[3]:
         raise ValueError("q and k must be [B, L, Hq, D] and [B, L, Hk, D]")
     if q.dtype not in _IO:
@@ -726,40 +752,37 @@ def _qk_args(q, k, norm, q_weight, k_weight, eps, q_scale, inv_freq, pos, pos0, 
         raise ValueError("q and k must share their dtype")
     if norm not in _NORM:
         raise ValueError(f"norm must be one of {sorted(_NORM)}, got {norm!r}")
-    B, L, Hq, D = q.shape
+    (B, L, Hq, D), Hk = q.shape, k.shape[2]
     for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
-        if w is not None and (tuple(w.shape) != (D,) or w.dtype != torch.float32 or not w.is_contiguous()):
+        if w is not None and (w.shape != (D,) or w.dtype != torch.float32 or not w.is_contiguous()):
             raise ValueError(f"{name} must be a contiguous float32 [{D}] tensor")
-    R = 0
+    R, sp = 0, (0, 0)
     if inv_freq is not None:
         if inv_freq.dim() != 1 or inv_freq.dtype != torch.float64 or not inv_freq.is_contiguous():
             raise ValueError("inv_freq must be a contiguous float64 tensor of R / 2 entries")
         R = 2 * inv_freq.numel()
-    if pos is not None and (tuple(pos.shape) != (B, L) or pos.dtype != torch.int64):
+    if pos is not None and (pos.shape != (B, L) or pos.dtype != torch.int64):
         raise ValueError(f"pos must be an int64 [{B}, {L}] tensor")
     if R == 0:
         pos = None
-    sh = _lib.SfQkShape()
-    sh.B, sh.L, sh.Hq, sh.Hk, sh.D = B, L, Hq, k.shape[2], D
-    sh.io_dtype, sh.norm, sh.R, sh.interleaved = _IO[q.dtype], _NORM[norm], R, int(bool(interleaved))
-    sh.eps, sh.q_scale, sh.pos0 = float(eps), float(q_scale), int(pos0)
-    if pos is not None:
-        sh.sp_b, sh.sp_l = pos.stride()
-    tensors = dict(q=q, k=k, q_weight=q_weight, k_weight=k_weight, inv_freq=inv_freq, pos=pos)
-    for names, pair in ((("yq", "yk"), ys), (("dq", "dk"), ds)):
-        for name, x, t in zip(names, (q, k), pair):
-            if t is not None and (t.shape != x.shape or t.dtype != x.dtype):
-                raise ValueError(f"{name} must match its input in shape and dtype")
-            tensors[name] = t
-            st = getattr(sh, name)
-            st.b, st.l, st.h = (L * x.shape[2] * D, x.shape[2] * D, D) if t is None else t.stride()[:3]
-    for name, x in tensors.items():
-        if x is not None and x.dim() == 4 and x.stride(3) != 1:
+    elif pos is not None:
+        sp = pos.stride()
+    strides = []
+    for name, x, t in (("q", q, q), ("k", k, k), ("yq", q, ys[0]), ("yk", k, ys[1]), ("dq", q, ds[0]),
+                       ("dk", k, ds[1])):
+        if t is None:
+            strides.append(_lib.SfStrides(L * x.shape[2] * D, x.shape[2] * D, D))
+            continue
+        if t is not x and (t.shape != x.shape or t.dtype != x.dtype):
+            raise ValueError(f"{name} must match its input in shape and dtype")
+        st = t.stride()
+        if st[3] != 1:
             raise ValueError(f"{name} must have a contiguous channel dim")
-    for st, x in ((sh.q, q), (sh.k, k)):
-        st.b, st.l, st.h = x.stride()[:3]
-    _on_gpu(q, **tensors)
-    return sh, pos
+        strides.append(_lib.SfStrides(*st[:3]))
+    dev = _on_gpu(q, k, q_weight, k_weight, inv_freq, pos, *ys, *ds)
+    sh = _lib.SfQkShape(B, Hq, Hk, D, L, _IO[q.dtype], _NORM[norm], R, 1 if interleaved else 0, eps, q_scale, pos0,
+                        *sp, *strides)
+    return dev, sh, pos
 
 
 def _packed(x):
@@ -778,22 +801,23 @@ def qk_norm_fwd(q, k, *, norm="l2", q_weight=None, k_weight=None, eps=1e-6, q_sc
     [B, L], or None for pos0 + l (pos0: where a segment begins); interleaved: pairs are
     channels (2i, 2i + 1) instead of (i, i + R / 2).  D: a multiple of 16 up to 256;
     R: of 16 up to D.  out=(q', k') supplies the outputs, slices of wider rows too."""
-    ys = (None, None) if out is None else out
-    sh, pos = _qk_args(q, k, norm, q_weight, k_weight, eps, q_scale, inv_freq, pos, pos0, interleaved, ys,
-                       (None, None))
-    stream = stream or torch.cuda.current_stream(q.device)
-    with torch.cuda.stream(stream):
-        yq, yk = (_packed(q), _packed(k)) if out is None else out
-        rc = _lib.lib().sf_qk_norm_fwd(ctypes.byref(sh), _ptr(q), _ptr(k), _ptr(q_weight), _ptr(k_weight),
-                                       _ptr(inv_freq), _ptr(pos), _ptr(yq), _ptr(yk),
-                                       ctypes.byref(_tuning(timing=timing)), _stream_handle(stream))
+    yq, yk = (None, None) if out is None else out
+    dev, sh, pos = _qk_args(q, k, norm, q_weight, k_weight, eps, q_scale, inv_freq, pos, pos0, interleaved, (yq, yk),
+                            (None, None))
+    ctx, handle = _on(dev, stream)
+    with ctx:
+        if out is None:
+            yq, yk = _packed(q), _packed(k)
+        rc = _lib.lib().sf_qk_norm_fwd(ctypes.byref(sh), q.data_ptr(), k.data_ptr(), _addr(q_weight),
+                                       _addr(k_weight), _addr(inv_freq), _addr(pos), yq.data_ptr(), yk.data_ptr(),
+                                       _timed(timing), handle)
     _lib.check("sf_qk_norm_fwd", rc)
     return yq, yk
 
 
 def qk_norm_bwd_workspace_bytes(q, k, dyq, dyk, weights=True):
     """Bytes of the workspace that qk_norm_bwd takes as out[4] (0 without weights)."""
-    sh, _ = _qk_args(q, k, "l2", None, None, 1e-6, 1.0, None, None, 0, False, (dyq, dyk), (None, None))
+    _, sh, _ = _qk_args(q, k, "l2", None, None, 1e-6, 1.0, None, None, 0, False, (dyq, dyk), (None, None))
     return _lib.lib().sf_qk_norm_bwd_workspace_bytes(ctypes.byref(sh), int(bool(weights)))
 
 
@@ -805,23 +829,23 @@ def qk_norm_bwd(q, k, dyq, dyk, *, norm="l2", q_weight=None, k_weight=None, eps=
     outputs (the last three None without weights)."""
     dq, dk, dwq, dwk, ws = (None,) * 5 if out is None else out
     weights = q_weight is not None
-    sh, pos = _qk_args(q, k, norm, q_weight, k_weight, eps, q_scale, inv_freq, pos, pos0, interleaved, (dyq, dyk),
-                       (dq, dk))
+    dev, sh, pos = _qk_args(q, k, norm, q_weight, k_weight, eps, q_scale, inv_freq, pos, pos0, interleaved, (dyq, dyk),
+                            (dq, dk))
     for name, t in (("dwq", dwq), ("dwk", dwk)):
         if t is not None and (tuple(t.shape) != (q.shape[3],) or t.dtype != torch.float32 or not t.is_contiguous()):
             raise ValueError(f"{name} must be a contiguous float32 [{q.shape[3]}] tensor")
-    _on_gpu(q, dwq=dwq, dwk=dwk, workspace=ws)
-    stream = stream or torch.cuda.current_stream(q.device)
+    _on_gpu(q, dwq, dwk, ws)
     L_ = _lib.lib()
-    with torch.cuda.stream(stream):
+    ctx, handle = _on(dev, stream)
+    with ctx:
         if out is None:
             dq, dk = _packed(q), _packed(k)
             if weights:
                 dwq, dwk = (torch.empty(q.shape[3], dtype=torch.float32, device=q.device) for _ in range(2))
                 ws = _ws(L_.sf_qk_norm_bwd_workspace_bytes(ctypes.byref(sh), 1), q.device)
-        rc = L_.sf_qk_norm_bwd(ctypes.byref(sh), _ptr(q), _ptr(k), _ptr(q_weight), _ptr(k_weight), _ptr(inv_freq),
-                               _ptr(pos), _ptr(dyq), _ptr(dyk), _ptr(dq), _ptr(dk), _ptr(dwq), _ptr(dwk), _ptr(ws),
-                               0 if ws is None else ws.numel() * ws.element_size(),
-                               ctypes.byref(_tuning(timing=timing)), _stream_handle(stream))
+        rc = L_.sf_qk_norm_bwd(ctypes.byref(sh), q.data_ptr(), k.data_ptr(), _addr(q_weight), _addr(k_weight),
+                               _addr(inv_freq), _addr(pos), dyq.data_ptr(), dyk.data_ptr(), dq.data_ptr(),
+                               dk.data_ptr(), _addr(dwq), _addr(dwk), _addr(ws),
+                               0 if ws is None else ws.numel() * ws.element_size(), _timed(timing), handle)
     _lib.check("sf_qk_norm_bwd", rc)
     return dq, dk, dwq, dwk

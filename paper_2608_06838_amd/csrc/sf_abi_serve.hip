@@ -174,7 +174,7 @@ sf_status check_qk(const sf_qk_shape *s, bool bwd) {
     return check_in("pos", {{s->B, s->sp_b}, {s->L, s->sp_l}}, 8, 8);
 }
 
-sf::QkArgs qk_args(const sf_qk_shape &s, bool bwd) {
+sf::QkArgs qk_args(const sf_qk_shape &s, bool bwd, bool weights) {
     sf::QkArgs a{};
     a.B = s.B;
     a.Hq = s.Hq;
@@ -197,12 +197,12 @@ sf::QkArgs qk_args(const sf_qk_shape &s, bool bwd) {
     a.syk = bwd ? s.dk : s.yk;
     a.sdyq = s.yq;
     a.sdyk = s.yk;
-    sf::qk_plan(a, bwd, device_cus());
+    sf::qk_plan(a, bwd, weights, device_cus());
     return a;
 }
 // a workgroup's part of dwq and dwk, for every workgroup
 size_t qk_ws_bytes(const sf_qk_shape &s, bool weights) {
-    return weights && s.B * s.L > 0 ? (size_t)qk_args(s, true).blocks * 2 * (size_t)s.D * 4 : 0;
+    return weights && s.B * s.L > 0 ? (size_t)qk_args(s, true, true).blocks * 2 * (size_t)s.D * 4 : 0;
 }
 sf_status check_qk_weights(const float *wq, const float *wk) {
     if (!wq != !wk) return fail(SF_E_NULL, "wq and wk go together");
@@ -383,7 +383,7 @@ sf_status sf_qk_norm_fwd(const sf_qk_shape *shape, const void *q, const void *k,
                             span(s.R ? inv_freq : nullptr, 4 * (int64_t)s.R, "inv_freq"),
                             strided(s.R ? pos : nullptr, {{s.B, s.sp_b}, {s.L, s.sp_l}}, 1, 8, "pos")},
                            {}));
-        sf::QkArgs a = qk_args(s, false);
+        sf::QkArgs a = qk_args(s, false, wq != nullptr);
         a.q = q;
         a.k = k;
         a.wq = wq;
@@ -439,7 +439,7 @@ sf_status sf_qk_norm_bwd(const sf_qk_shape *shape, const void *q, const void *k,
                             strided(s.R ? pos : nullptr, {{s.B, s.sp_b}, {s.L, s.sp_l}}, 1, 8, "pos")},
                            {span(weights ? dwq : nullptr, nw, "dwq"), span(weights ? dwk : nullptr, nw, "dwk"),
                             wsrange(need ? ws : nullptr, need)}));
-        sf::QkArgs a = qk_args(s, true);
+        sf::QkArgs a = qk_args(s, true, weights);
         a.q = q;
         a.k = k;
         a.dyq = dyq;

@@ -209,18 +209,24 @@ struct QkArgs {
     int64_t L, pos0, sp_b, sp_l;
     sf_strides sq, sk, syq, syk, sdyq, sdyk;
 };
-constexpr int QK_W = 4, QK_U = 4, QK_UB = 2;  // waves of a workgroup; row groups in flight, forward and backward
+constexpr int QK_W = 4;  // waves of a workgroup
+// workgroups that share a CU (the weights' gradients take registers)
+constexpr int qk_resident(bool bwd, bool weights) { return bwd && weights ? 3 : 4; }
+// row groups a wave has in flight, twice over: 64 bytes a lane, which fits the registers
+constexpr int qk_groups(bool bwd, size_t elem) { return (int)((bwd ? 4 : 8) / elem); }
 // parts and blocks of a launch, from the shape
-inline void qk_plan(QkArgs &a, bool bwd, int n_cu) {
+inline void qk_plan(QkArgs &a, bool bwd, bool weights, int n_cu) {
     int lpr = 2;  // lanes of a row
     while (8 * lpr < a.D) lpr *= 2;
-    const int rows = 64 / lpr * (bwd ? QK_UB : QK_U);
+    const int rows = 64 / lpr * qk_groups(bwd, a.io == SF_BF16 ? 2 : 4);
     const int groups = (a.Hq + rows - 1) / rows + (a.Hk + rows - 1) / rows;
     // a token's row groups are shared between waves until the launch has eight a CU
     a.parts = 1;
     while (a.parts < groups && (int64_t)a.n_tok * a.parts < 8 * (int64_t)n_cu) ++a.parts;
-    const int64_t units = (int64_t)a.n_tok * a.parts, blocks = (units + QK_W - 1) / QK_W, most = 8 * (int64_t)n_cu;
-    a.blocks = (int32_t)(blocks < most ? blocks : most);
+    // no more workgroups than the CUs hold, each wave with the same number of tokens, or one less
+    const int64_t units = (int64_t)a.n_tok * a.parts, most = qk_resident(bwd, weights) * (int64_t)n_cu * QK_W;
+    const int64_t each = (units + most - 1) / most;
+    a.blocks = each ? (int32_t)(((units + each - 1) / each + QK_W - 1) / QK_W) : 0;
 }
 hipError_t launch_qk(bool bwd, const QkArgs &a, hipStream_t s, hipEvent_t e0, hipEvent_t e1);
 

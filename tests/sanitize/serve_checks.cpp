@@ -264,7 +264,7 @@ int main() {
                 const sf::QkArgs &a = rec.qk.back().second;
                 EXPECT(rec.qk.back().first && a.blocks >= 1 && a.parts >= 1);
                 EXPECT(c.ws_bytes == (size_t)a.blocks * 2 * D * 4);
-                EXPECT((int64_t)a.blocks * sf::QK_W >= (int64_t)n * a.parts || a.blocks == 8 * a.B * 256);
+                EXPECT(a.blocks <= 4 * 256 && a.parts <= 2 * Hq + 2);
             }
     if (failures) return 1;
     std::printf("serve checks passed\n");

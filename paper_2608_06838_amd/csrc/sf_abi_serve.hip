@@ -354,7 +354,7 @@ sf_status sf_conv_ragged_fwd(const sf_conv_ragged_shape *shape, const sf_ragged 
         a.W = s.W;
         a.act = s.act;
         a.io = s.io_dtype;
-        a.run = 8;
+        a.run = sf::conv_ragged_run(b.T, b.N, s.C, device_cus());
         a.n_runs = b.T / a.run + b.N;
         a.sx_t = s.sx_t;
         a.sy_t = s.sy_t;

@@ -191,6 +191,14 @@ struct ConvRaggedArgs {
     int64_t n_runs;  // upper bound of the runs: T / run + N
     int64_t sx_t, sy_t, ss;
 };
+// Tokens of a run: 32 keep the halo rows, read twice, under a tenth (8259 tokens of
+// 15360 channels: runs of 8 143 us, 16 129, 32 127, 64 134), 8 (one load group) where
+// longer ones would leave the chip short of threads (CONV_FILL).
+inline int conv_ragged_run(int64_t T, int64_t N, int64_t C, int n_cu) {
+    int run = 32;
+    while (run > CONV_G && (T / run + N) * (C / CONV_E) < CONV_FILL * n_cu) run /= 2;
+    return run;
+}
 hipError_t launch_conv_ragged(const ConvRaggedArgs &a, hipStream_t s, hipEvent_t e0, hipEvent_t e1);
 
 // Norms and rotation of queries and keys (sf_qk.hip).

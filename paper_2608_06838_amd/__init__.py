@@ -689,7 +689,7 @@ def gdn_ragged_fwd(q, k, v, g, beta, state, cu_seqlens, slots=None, *, fresh=Non
     with ctx:
         nbytes = 0 if ws is None else ws.numel() * ws.element_size()
         if out is None:
-            o = torch.empty(v.shape, dtype=v.dtype, device=v.device)
+            o = v.new_empty(v.shape)
             nbytes = L_.sf_gdn_ragged_workspace_bytes(ctypes.byref(sh), ctypes.byref(b))
             ws = _ws(nbytes, v.device) if nbytes else None
         rc = L_.sf_gdn_ragged_fwd(ctypes.byref(sh), ctypes.byref(b), q.data_ptr(), k.data_ptr(), v.data_ptr(),
@@ -731,7 +731,7 @@ def conv_ragged_fwd(x, w, tails, cu_seqlens, slots=None, *, fresh=None, act="sil
                                 0 if tails is None else tails.stride(0))
     ctx, handle = _on(dev, stream)
     with ctx:
-        y = torch.empty((T, C), dtype=x.dtype, device=x.device) if out is None else out
+        y = x.new_empty((T, C)) if out is None else out
         rc = _lib.lib().sf_conv_ragged_fwd(ctypes.byref(sh), ctypes.byref(b), x.data_ptr(), w.data_ptr(),
                                            _addr(tails), y.data_ptr(), _timed(timing), handle)
     _lib.check("sf_conv_ragged_fwd", rc)
@@ -741,52 +741,56 @@ def conv_ragged_fwd(x, w, tails, cu_seqlens, slots=None, *, fresh=None, act="sil
 _NORM = {"none": _lib.SF_NORM_NONE, "l2": _lib.SF_NORM_L2, "rms": _lib.SF_NORM_RMS}
 
 
-def _qk_args(q, k, norm, q_weight, k_weight, eps, q_scale, inv_freq, pos, pos0, interleaved, ys, ds):
-    """(device, shape of the call, pos); ys: outputs or their gradients, ds: the inputs'
-    gradients (None: packed)."""
-    if q.dim() != 4 or k.dim() != 4 or q.shape[:2] != k.shape[:2] or q.shape[3] != k.shape[3]:
+def _qk_strides(name, t, x, dtype, packed):
+    """Strides of an output or a gradient that goes with input x (None: packed)."""
+    if t is None:
+        return packed
+    st = t.stride()
+    if t.shape != x.shape or t.dtype != dtype or st[3] != 1:
+        raise ValueError(f"{name} must match its input in shape and dtype, its channels contiguous")
+    return st[:3]
+
+
+def _qk_args(q, k, norm, q_weight, k_weight, eps, q_scale, inv_freq, pos, pos0, interleaved, yq, yk, dq, dk):
+    """(device, shape of the call, pos); yq, yk: outputs or their gradients, dq, dk: the
+    inputs' gradients (None: packed)."""
+    if q.dim() != 4 or k.dim() != 4:
         raise ValueError("q and k must be [B, L, Hq, D] and [B, L, Hk, D]")
-    if q.dtype not in _IO:
-        raise TypeError(f"unsupported I/O dtype {q.dtype}")
-    if k.dtype != q.dtype:
-        raise ValueError("q and k must share their dtype")
+    dtype, (B, L, Hq, D), Hk = q.dtype, q.shape, k.shape[2]
+    if dtype not in _IO:
+        raise TypeError(f"unsupported I/O dtype {dtype}")
+    if k.shape != (B, L, Hk, D) or k.dtype != dtype:
+        raise ValueError("q and k must share batch, tokens, channels and dtype")
     if norm not in _NORM:
         raise ValueError(f"norm must be one of {sorted(_NORM)}, got {norm!r}")
-    (B, L, Hq, D), Hk = q.shape, k.shape[2]
-    for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
-        if w is not None and (w.shape != (D,) or w.dtype != torch.float32 or not w.is_contiguous()):
-            raise ValueError(f"{name} must be a contiguous float32 [{D}] tensor")
+    if q_weight is not None or k_weight is not None:
+        for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
+            if w is None or w.shape != (D,) or w.dtype != torch.float32 or not w.is_contiguous():
+                raise ValueError(f"{name} must be a contiguous float32 [{D}] tensor (both weights or neither)")
     R, sp = 0, (0, 0)
     if inv_freq is not None:
         if inv_freq.dim() != 1 or inv_freq.dtype != torch.float64 or not inv_freq.is_contiguous():
             raise ValueError("inv_freq must be a contiguous float64 tensor of R / 2 entries")
         R = 2 * inv_freq.numel()
-    if pos is not None and (pos.shape != (B, L) or pos.dtype != torch.int64):
-        raise ValueError(f"pos must be an int64 [{B}, {L}] tensor")
-    if R == 0:
-        pos = None
-    elif pos is not None:
-        sp = pos.stride()
-    strides = []
-    for name, x, t in (("q", q, q), ("k", k, k), ("yq", q, ys[0]), ("yk", k, ys[1]), ("dq", q, ds[0]),
-                       ("dk", k, ds[1])):
-        if t is None:
-            strides.append(_lib.SfStrides(L * x.shape[2] * D, x.shape[2] * D, D))
-            continue
-        if t is not x and (t.shape != x.shape or t.dtype != x.dtype):
-            raise ValueError(f"{name} must match its input in shape and dtype")
-        st = t.stride()
-        if st[3] != 1:
-            raise ValueError(f"{name} must have a contiguous channel dim")
-        strides.append(_lib.SfStrides(*st[:3]))
-    dev = _on_gpu(q, k, q_weight, k_weight, inv_freq, pos, *ys, *ds)
-    sh = _lib.SfQkShape(B, Hq, Hk, D, L, _IO[q.dtype], _NORM[norm], R, 1 if interleaved else 0, eps, q_scale, pos0,
-                        *sp, *strides)
-    return dev, sh, pos
+    if pos is not None:
+        if pos.shape != (B, L) or pos.dtype != torch.int64:
+            raise ValueError(f"pos must be an int64 [{B}, {L}] tensor")
+        if R:
+            sp = pos.stride()
+        else:
+            pos = None
+    sq, sk, pq, pk = q.stride(), k.stride(), (L * Hq * D, Hq * D, D), (L * Hk * D, Hk * D, D)
+    if sq[3] != 1 or sk[3] != 1:
+        raise ValueError("q and k must have a contiguous channel dim")
+    dev = _on_gpu(q, k, q_weight, k_weight, inv_freq, pos, yq, yk, dq, dk)
+    return dev, _lib.SfQkShape(
+        B, Hq, Hk, D, L, _IO[dtype], _NORM[norm], R, 1 if interleaved else 0, eps, q_scale, pos0, sp[0], sp[1],
+        sq[:3], sk[:3], _qk_strides("yq", yq, q, dtype, pq), _qk_strides("yk", yk, k, dtype, pk),
+        _qk_strides("dq", dq, q, dtype, pq), _qk_strides("dk", dk, k, dtype, pk)), pos
 
 
 def _packed(x):
-    return torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    return x.new_empty(x.shape)
 
 
 def qk_norm_fwd(q, k, *, norm="l2", q_weight=None, k_weight=None, eps=1e-6, q_scale=1.0, inv_freq=None, pos=None,
@@ -802,8 +806,8 @@ def qk_norm_fwd(q, k, *, norm="l2", q_weight=None, k_weight=None, eps=1e-6, q_sc
     channels (2i, 2i + 1) instead of (i, i + R / 2).  D: a multiple of 16 up to 256;
     R: of 16 up to D.  out=(q', k') supplies the outputs, slices of wider rows too."""
     yq, yk = (None, None) if out is None else out
-    dev, sh, pos = _qk_args(q, k, norm, q_weight, k_weight, eps, q_scale, inv_freq, pos, pos0, interleaved, (yq, yk),
-                            (None, None))
+    dev, sh, pos = _qk_args(q, k, norm, q_weight, k_weight, eps, q_scale, inv_freq, pos, pos0, interleaved, yq, yk,
+                            None, None)
     ctx, handle = _on(dev, stream)
     with ctx:
         if out is None:
@@ -817,7 +821,7 @@ def qk_norm_fwd(q, k, *, norm="l2", q_weight=None, k_weight=None, eps=1e-6, q_sc
 
 def qk_norm_bwd_workspace_bytes(q, k, dyq, dyk, weights=True):
     """Bytes of the workspace that qk_norm_bwd takes as out[4] (0 without weights)."""
-    _, sh, _ = _qk_args(q, k, "l2", None, None, 1e-6, 1.0, None, None, 0, False, (dyq, dyk), (None, None))
+    _, sh, _ = _qk_args(q, k, "l2", None, None, 1e-6, 1.0, None, None, 0, False, dyq, dyk, None, None)
     return _lib.lib().sf_qk_norm_bwd_workspace_bytes(ctypes.byref(sh), int(bool(weights)))
 
 
@@ -829,19 +833,20 @@ def qk_norm_bwd(q, k, dyq, dyk, *, norm="l2", q_weight=None, k_weight=None, eps=
     outputs (the last three None without weights)."""
     dq, dk, dwq, dwk, ws = (None,) * 5 if out is None else out
     weights = q_weight is not None
-    dev, sh, pos = _qk_args(q, k, norm, q_weight, k_weight, eps, q_scale, inv_freq, pos, pos0, interleaved, (dyq, dyk),
-                            (dq, dk))
-    for name, t in (("dwq", dwq), ("dwk", dwk)):
+    dev, sh, pos = _qk_args(q, k, norm, q_weight, k_weight, eps, q_scale, inv_freq, pos, pos0, interleaved, dyq, dyk,
+                            dq, dk)
+    for name, t in (("dwq", dwq), ("dwk", dwk)) if out is not None else ():
         if t is not None and (tuple(t.shape) != (q.shape[3],) or t.dtype != torch.float32 or not t.is_contiguous()):
             raise ValueError(f"{name} must be a contiguous float32 [{q.shape[3]}] tensor")
-    _on_gpu(q, dwq, dwk, ws)
+    if out is not None:
+        _on_gpu(q, dwq, dwk, ws)
     L_ = _lib.lib()
     ctx, handle = _on(dev, stream)
     with ctx:
         if out is None:
             dq, dk = _packed(q), _packed(k)
             if weights:
-                dwq, dwk = (torch.empty(q.shape[3], dtype=torch.float32, device=q.device) for _ in range(2))
+                dwq, dwk = q.new_empty((2, q.shape[3]), dtype=torch.float32).unbind()
                 ws = _ws(L_.sf_qk_norm_bwd_workspace_bytes(ctypes.byref(sh), 1), q.device)
         rc = L_.sf_qk_norm_bwd(ctypes.byref(sh), q.data_ptr(), k.data_ptr(), _addr(q_weight), _addr(k_weight),
                                _addr(inv_freq), _addr(pos), dyq.data_ptr(), dyk.data_ptr(), dq.data_ptr(),

@@ -161,7 +161,13 @@ inline int64_t gdn_token_waves(const GdnRaggedArgs &a) { return (int64_t)a.r.N *
 // planes (exact), P in two, six fragments of 1 KB a plane, then the chunk's e^b,
 // e^(b_63 - b) and beta (sf_ragged_chunk.hip)
 constexpr int RAG_FRAGS = 6, RAG_TP = 3, RAG_PP = 2, RAG_SYS = ((RAG_TP + RAG_PP) * RAG_FRAGS + 1) * 1024;
-constexpr int RAG_LONG = 16;
+// Sequences up to so many tokens are taken token by token: a chunk costs the same
+// whatever its tokens, a token what the CUs' other waves leave it (20 heads of 128, us in
+// chunks / token by token: one sequence of 8 tokens 12.8 / 10.4, of 12 12.9 / 13.6, of 16
+// 12.9 / 17.3; 64 sequences of 16 tokens 86 / 70, of 24 91 / 95, of 32 91 / 120; 256 of 24
+// with 40 heads 674 / 648, of 32 696 / 826).
+constexpr int RAG_LONG = 24, RAG_LONG_FEW = 10;
+inline int gdn_long(const GdnRaggedArgs &a) { return gdn_token_waves(a) <= a.n_cu ? RAG_LONG_FEW : RAG_LONG; }
 // items of the walk with nc 16-column tiles each, for n sequences: (sequence, value
 // head) pairs in eights, their column blocks
 __host__ __device__ inline int64_t gdn_walk_items(const GdnRaggedArgs &a, int64_t n, int nc) {

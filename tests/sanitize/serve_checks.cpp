@@ -202,7 +202,7 @@ int main() {
     // a long sequence: the systems and the plan, then the walk with the other tokens
     EXPECT(rec.gdn.empty() && rec.prep.size() == 3 && rec.walk.size() == 3);
     EXPECT(rec.walk[0].Hv == 8 && rec.walk[0].r.N == 3 && rec.walk[1].sq_t == 0);
-    EXPECT(rec.walk[0].n_chunks == 100 / 64 + 3 && rec.walk[0].longer == sf::RAG_LONG);
+    EXPECT(rec.walk[0].n_chunks == 100 / 64 + 3 && rec.walk[0].longer == sf::RAG_LONG_FEW);
     EXPECT(sf::gdn_token_waves(rec.walk[0]) == 3 * 8 * 4);
     {
         Gdn c;
@@ -219,7 +219,7 @@ int main() {
         EXPECT(c.run() == SF_E_ALIAS);
         c.ws = nullptr;
         EXPECT(c.run() == SF_E_WORKSPACE);
-        c.b.max_len = sf::RAG_LONG;  // token by token: no workspace
+        c.b.max_len = sf::RAG_LONG_FEW;  // token by token: no workspace
         EXPECT(sf_gdn_ragged_workspace_bytes(&c.s, &c.b) == 0 && c.run() == SF_OK);
         c.b.max_len = 90, c.s.io_dtype = SF_F32;
         EXPECT(sf_gdn_ragged_workspace_bytes(&c.s, &c.b) == 0 && c.run() == SF_OK);

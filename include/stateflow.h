@@ -506,7 +506,7 @@ typedef struct sf_ragged {
  * (g, beta: 4), strides of q, k, v, o multiples of 16 bytes, ss a multiple of 4.
  * Inputs may be broadcast (stride 0).  No allocation, no synchronisation.
  * Short sequences, and all with SF_F32, run token by token; with SF_BF16 and a max_len
- * above 10 (24 where the launch has more than a wave a CU), longer ones run in chunks of
+ * above 12 (24 where the launch has more than a wave a CU), longer ones run in chunks of
  * 64 tokens, which takes the workspace (contents on entry ignored, 16-byte aligned).
  */
 typedef struct sf_gdn_ragged_shape {

@@ -300,7 +300,7 @@ sf_status sf_gdn_ragged_fwd(const sf_gdn_ragged_shape *shape, const sf_ragged *b
         a.o = o;
         a.ws = (char *)ws;
         a.plan = need ? (int32_t *)(a.ws + sf::gdn_plan_at(a)) : nullptr;
-        const double tok = (double)sf::gdn_token_waves(a);
+        const double tok = (double)sf::gdn_token_waves(a);  // workgroups hold four
         TRY(grid_fits(std::max(tok + sf::gdn_walk_groups(a), (double)a.n_chunks * s.Hk + 1)));
         sf_timing *const tm = timing_of(tuning);
         hipEvent_t e0, e1;

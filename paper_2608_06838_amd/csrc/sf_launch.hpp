@@ -154,19 +154,23 @@ struct GdnRaggedArgs {
     char *ws;          // chunk systems: [n_chunks][Hv] of RAG_SYS bytes
     int32_t *plan;     // [2 + N], see gdn_plan_at
 };
-// waves of the token-by-token kernel: one for each sequence, value head and tile of 4 TOK_CL columns
-constexpr int TOK_CL = 8;
-inline int64_t gdn_token_waves(const GdnRaggedArgs &a) { return (int64_t)a.r.N * a.Hv * (a.Dv / (4 * TOK_CL)); }
+// waves of the token-by-token kernel: one for each sequence, value head and tile of 4 cl
+// columns.  TOK_CL column lanes take whole 128-byte lines of the state; half of them make
+// a token cheaper for a wave, and pay while there is a SIMD for each (16 tokens of 20
+// heads of 128, us with 8 / 4 lanes: one sequence 17.8 / 14.4, 8 sequences 19.6 / 21.5,
+// 64 67 / 85): launches of at most TOK_FEW full waves a CU.
+constexpr int TOK_CL = 8, TOK_FEW = 2;
+inline int64_t gdn_token_waves(const GdnRaggedArgs &a, int cl = TOK_CL) { return (int64_t)a.r.N * a.Hv * (a.Dv / (4 * cl)); }
 // A chunk's triangular system, as operand fragments: T = (I + A)^-1 in three bf16
 // planes (exact), P in two, six fragments of 1 KB a plane, then the chunk's e^b,
 // e^(b_63 - b) and beta (sf_ragged_chunk.hip)
 constexpr int RAG_FRAGS = 6, RAG_TP = 3, RAG_PP = 2, RAG_SYS = ((RAG_TP + RAG_PP) * RAG_FRAGS + 1) * 1024;
 // Sequences up to so many tokens are taken token by token: a chunk costs the same
 // whatever its tokens, a token what the CUs' other waves leave it (20 heads of 128, us in
-// chunks / token by token: one sequence of 8 tokens 12.8 / 10.4, of 12 12.9 / 13.6, of 16
-// 12.9 / 17.3; 64 sequences of 16 tokens 86 / 70, of 24 91 / 95, of 32 91 / 120; 256 of 24
-// with 40 heads 674 / 648, of 32 696 / 826).
-constexpr int RAG_LONG = 24, RAG_LONG_FEW = 10;
+// chunks / token by token: one sequence of 8 tokens 12.8 / 8.9, of 12 12.9 / 11.7, of 16
+// 12.9 / 14.4; 64 sequences of 16 tokens 86 / 67, of 24 91 / 89, of 32 91 / 114; 256 of 24
+// with 40 heads 674 / 637, of 32 696 / 839).
+constexpr int RAG_LONG = 24, RAG_LONG_FEW = 12;
 inline int gdn_long(const GdnRaggedArgs &a) { return gdn_token_waves(a) <= a.n_cu ? RAG_LONG_FEW : RAG_LONG; }
 // items of the walk with nc 16-column tiles each, for n sequences: (sequence, value
 // head) pairs in eights, their column blocks

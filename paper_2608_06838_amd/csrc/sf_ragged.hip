@@ -13,16 +13,16 @@ namespace sf {
 namespace {
 
 // ------------------------------------------------- gated delta rule, token by token
-template <typename T, int DK>
+template <typename T, int DK, int CL>
 __global__ void __launch_bounds__(TOK_NT) k_gdn_tokens(GdnRaggedArgs a) {
-    gdn_tokens<T, DK, TOK_CL>(a, (int64_t)blockIdx.x * (TOK_NT / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6));
+    gdn_tokens<T, DK, CL>(a, (int64_t)blockIdx.x * (TOK_NT / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6));
 }
 
-template <typename T>
+template <typename T, int CL>
 hipError_t gdn_tokens_t(const GdnRaggedArgs &a, hipStream_t s, hipEvent_t e0, hipEvent_t e1) {
-    const dim3 grid((unsigned)((gdn_token_waves(a) + TOK_NT / 64 - 1) / (TOK_NT / 64)));
-    if (a.Dk == 128) hipExtLaunchKernelGGL((k_gdn_tokens<T, 128>), grid, dim3(TOK_NT), 0, s, e0, e1, 0, a);
-    else hipExtLaunchKernelGGL((k_gdn_tokens<T, 64>), grid, dim3(TOK_NT), 0, s, e0, e1, 0, a);
+    const dim3 grid((unsigned)((gdn_token_waves(a, CL) + TOK_NT / 64 - 1) / (TOK_NT / 64)));
+    if (a.Dk == 128) hipExtLaunchKernelGGL((k_gdn_tokens<T, 128, CL>), grid, dim3(TOK_NT), 0, s, e0, e1, 0, a);
+    else hipExtLaunchKernelGGL((k_gdn_tokens<T, 64, CL>), grid, dim3(TOK_NT), 0, s, e0, e1, 0, a);
     return hipGetLastError();
 }
 
@@ -174,7 +174,9 @@ hipError_t conv_ragged_t(const ConvRaggedArgs &a, hipStream_t s, hipEvent_t e0, 
 }  // namespace
 
 hipError_t launch_gdn_tokens(const GdnRaggedArgs &a, hipStream_t s, hipEvent_t e0, hipEvent_t e1) {
-    return a.io == SF_BF16 ? gdn_tokens_t<__bf16>(a, s, e0, e1) : gdn_tokens_t<float>(a, s, e0, e1);
+    if (gdn_token_waves(a, TOK_CL) <= TOK_FEW * (int64_t)a.n_cu)
+        return a.io == SF_BF16 ? gdn_tokens_t<__bf16, TOK_CL / 2>(a, s, e0, e1) : gdn_tokens_t<float, TOK_CL / 2>(a, s, e0, e1);
+    return a.io == SF_BF16 ? gdn_tokens_t<__bf16, TOK_CL>(a, s, e0, e1) : gdn_tokens_t<float, TOK_CL>(a, s, e0, e1);
 }
 
 hipError_t launch_conv_ragged(const ConvRaggedArgs &a, hipStream_t s, hipEvent_t e0, hipEvent_t e1) {

@@ -508,6 +508,8 @@ typedef struct sf_ragged {
  * Short sequences, and all with SF_F32, run token by token; with SF_BF16 and a max_len
  * above 12 (24 where the launch has more than a wave a CU), longer ones run in chunks of
  * 64 tokens, which takes the workspace (contents on entry ignored, 16-byte aligned).
+ * g = -inf forgets the state.  A NaN or infinity elsewhere spoils its own sequence, from
+ * its token on or from the start of that token's chunk, and no other.
  */
 typedef struct sf_gdn_ragged_shape {
     int32_t Hk, Hv, Dk, Dv;

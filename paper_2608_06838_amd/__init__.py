@@ -604,6 +604,8 @@ def _on(dev, stream):
     """(context in which the call's tensors are allocated and its kernels launched, the
     stream's handle)."""
     if stream is not None:
+        if stream.device.index != dev:
+            raise ValueError(f"the stream is on {stream.device}, the tensors on cuda:{dev}")
         return torch.cuda.stream(stream), stream.cuda_stream
     ctx = contextlib.nullcontext() if torch.cuda.current_device() == dev else torch.cuda.device(dev)
     return ctx, torch.cuda.current_stream(dev).cuda_stream

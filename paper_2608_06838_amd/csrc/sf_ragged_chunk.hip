@@ -81,8 +81,8 @@ __device__ __forceinline__ void split3(const f32x4 &a, const f32x4 &b, bf16x8 &h
 }
 
 // e^-104 is below the smallest fp32: a gate of -inf (forget everything) becomes one
-// whose running sum stays finite
-__device__ __forceinline__ float gate_log2(float g) { return fmaxf(g, -104.f) * LOG2E; }
+// whose running sum stays finite (and NaN stays NaN)
+__device__ __forceinline__ float gate_log2(float g) { return (g < -104.f ? -104.f : g) * LOG2E; }
 
 // Rows [0, 64) of a chunk tile of D channels, in 16-byte blocks over NT threads, rows
 // from m on the last one again; to LDS with pitch LD, rows of bit 3 swizzled by SW channels (see

@@ -253,6 +253,60 @@ def test_gdn_far_slots_and_rows():
         close("state", pool, want_S, DELTA)
 
 
+def test_gdn_far_rows_in_chunks():
+    """A long sequence whose slot and rows lie more than 2^32 bytes in, in chunks."""
+    print("[gdn ragged] far offsets, chunks", flush=True)
+    lens = [500, 1, 99]
+    cu, T = ref.sequences(lens)
+    q, k, v, g, beta, state = gdn_inputs(T, 1, 1, 64, 64, 3, seed=19)
+    pool = torch.empty(3, 1, 300000, 64, 64, device=DEV)[:, :, 0]
+    pool.copy_(state)
+    wide = torch.empty(T, 4000000, dtype=torch.bfloat16, device=DEV)  # 8 MB rows, 4.8 GB
+    qs, ks, vs = (wide[:, a:a + 64].unflatten(1, (1, 64)) for a in (0, 64, 128))
+    for a, b in ((qs, q), (ks, k), (vs, v)):
+        a.copy_(b)
+    slots = [0, -1, 2]
+    want_o, written, want_S = ref.gdn(q, k, v, g, beta, state, cu, slots)
+    out = torch.empty(T, 1, 4000000, dtype=torch.bfloat16, device=DEV)[..., :64]
+    ws = torch.empty(sf.gdn_ragged_workspace_bytes(qs, ks, vs, g, beta, pool, i32(cu), i32(slots), max_len=500),
+                     dtype=torch.uint8, device=DEV)
+    assert ws.numel() > 0  # the chunks' systems: this call takes them
+    sf.gdn_ragged_fwd(qs, ks, vs, g, beta, pool, i32(cu), i32(slots), max_len=500, out=(out, ws))
+    torch.cuda.synchronize()
+    w = torch.tensor(written, device=DEV)
+    close("o", out[w], want_o[written], DELTA)
+    close("state", pool[[0, 2]], want_S[[0, 2]], DELTA)
+    assert torch.equal(pool[1], state[1])
+
+
+def test_gdn_nan_stays_in_its_sequence():
+    """A NaN gate or value reaches its own sequence's state and no other's."""
+    lens = [70, 90, 3, 2]
+    cu, T = ref.sequences(lens)
+    print("[gdn ragged] NaN", flush=True)
+    args = gdn_inputs(T, 1, 2, 64, 64, 4, seed=20)
+    args[3][30] = float("nan")
+    args[2][161] = float("nan")
+    for max_len in (1, 90):
+        S = args[5].clone()
+        o = sf.gdn_ragged_fwd(*args[:5], S, i32(cu), max_len=max_len)
+        torch.cuda.synchronize()
+        assert bool(S[0].isnan().all()) and bool(S[2].isnan().all())
+        assert bool(o[69].isnan().all()) and bool(o[162].isnan().all())
+        assert bool(S[[1, 3]].isfinite().all()) and bool(o[70:160].isfinite().all()) and bool(o[163:].isfinite().all())
+
+
+def test_gdn_many_sequences_of_all_lengths():
+    """Sequences over every bucket of the plan up to 40 chunks, more items than workgroups
+    at once, in an order of their own; the longest in single column tiles."""
+    rng = np.random.RandomState(5)
+    lens = [int(n) for n in rng.randint(0, 200, 60)] + [2500, 0, 1, 24, 25, 12, 13, 640]
+    rng.shuffle(lens)
+    cu, T = ref.sequences(lens)
+    print(f"[gdn ragged] {len(lens)} sequences, {T} tokens", flush=True)
+    run_gdn(gdn_inputs(T, 1, 2, 64, 64, len(lens), seed=21), cu, max_len=2500)
+
+
 def test_gdn_streams_graph_and_repeat():
     """Runs on another stream, captured with its workspace and replayed, with eager calls
     between the replays; every run of one input gives the same bits."""
@@ -291,6 +345,23 @@ def test_gdn_streams_graph_and_repeat():
     torch.cuda.synchronize()
     close("o", o2[:108], want_o[:108], DELTA)
     close("state", args[5], want_S, DELTA)
+
+
+def test_stream_of_the_tensors_device():
+    """Two streams at once, each on slots of its own in one pool."""
+    cu, T = ref.sequences([70, 3])
+    print("[gdn ragged] two streams", flush=True)
+    args = gdn_inputs(T, 1, 2, 128, 64, 4, seed=22)
+    want = [ref.gdn(*args, cu, s) for s in ([0, 3], [2, 1])]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    outs = [sf.gdn_ragged_fwd(*args, i32(cu), i32(sl), max_len=70, stream=st)
+            for sl, st in zip(([0, 3], [2, 1]), streams)]
+    torch.cuda.synchronize()
+    for o, w in zip(outs, want):
+        close("o", o, w[0], DELTA)
+    close("state", args[5][[0, 3]], want[0][2][[0, 3]], DELTA)
+    close("state", args[5][[2, 1]], want[1][2][[2, 1]], DELTA)
 
 
 def test_gdn_empty_calls():

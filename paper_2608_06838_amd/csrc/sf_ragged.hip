@@ -31,7 +31,7 @@ hipError_t gdn_tokens_t(const GdnRaggedArgs &a, hipStream_t s, hipEvent_t e0, hi
 // tail.  Streaming work like the training form: a thread takes 8 consecutive channels
 // and a run of tokens of one sequence (find_seq).  The sequence's first run alone reads the old tail, and it writes the new one, after
 // that read, from the sequence's last rows, so the pool is updated in place with no
-// order between workgroups.
+// order between workgroups.  8259 tokens of 15360 channels: 104 us, 4.9 TB/s.
 constexpr int CR_NT = 256, CR_G = 8;  // threads; tokens loaded together
 
 // u sigmoid(u) by the hardware exp2 and reciprocal, one unit in the last place each

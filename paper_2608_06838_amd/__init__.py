@@ -600,12 +600,17 @@ def _on_gpu(ref, *ts):
     return dev
 
 
-def _on(dev, stream):
+def _on(dev, stream, *ts):
     """(context in which the call's tensors are allocated and its kernels launched, the
-    stream's handle)."""
+    stream's handle).  On a stream of its own the call keeps the memory of its tensors
+    from being handed out again before that stream has passed it."""
     if stream is not None:
         if stream.device.index != dev:
             raise ValueError(f"the stream is on {stream.device}, the tensors on cuda:{dev}")
+        if stream != torch.cuda.current_stream(dev):
+            for t in ts:
+                if t is not None:
+                    t.record_stream(stream)
         return torch.cuda.stream(stream), stream.cuda_stream
     ctx = contextlib.nullcontext() if torch.cuda.current_device() == dev else torch.cuda.device(dev)
     return ctx, torch.cuda.current_stream(dev).cuda_stream
@@ -687,7 +692,7 @@ def gdn_ragged_fwd(q, k, v, g, beta, state, cu_seqlens, slots=None, *, fresh=Non
     if ws is not None:
         _on_gpu(q, ws)
     L_ = _lib.lib()
-    ctx, handle = _on(dev, stream)
+    ctx, handle = _on(dev, stream, q, k, v, g, beta, state, cu_seqlens, slots, fresh, o, ws)
     with ctx:
         nbytes = 0 if ws is None else ws.numel() * ws.element_size()
         if out is None:
@@ -731,7 +736,7 @@ def conv_ragged_fwd(x, w, tails, cu_seqlens, slots=None, *, fresh=None, act="sil
         b.n_slots = 2 ** 31 - 1  # no tails: only negative slots are out of range
     sh = _lib.SfConvRaggedShape(C, W, _IO[x.dtype], _ACT[act], 0, x.stride(0), C if out is None else out.stride(0),
                                 0 if tails is None else tails.stride(0))
-    ctx, handle = _on(dev, stream)
+    ctx, handle = _on(dev, stream, x, w, tails, cu_seqlens, slots, fresh, out)
     with ctx:
         y = x.new_empty((T, C)) if out is None else out
         rc = _lib.lib().sf_conv_ragged_fwd(ctypes.byref(sh), ctypes.byref(b), x.data_ptr(), w.data_ptr(),
@@ -810,7 +815,7 @@ def qk_norm_fwd(q, k, *, norm="l2", q_weight=None, k_weight=None, eps=1e-6, q_sc
     yq, yk = (None, None) if out is None else out
     dev, sh, pos = _qk_args(q, k, norm, q_weight, k_weight, eps, q_scale, inv_freq, pos, pos0, interleaved, yq, yk,
                             None, None)
-    ctx, handle = _on(dev, stream)
+    ctx, handle = _on(dev, stream, q, k, q_weight, k_weight, inv_freq, pos, yq, yk)
     with ctx:
         if out is None:
             yq, yk = _packed(q), _packed(k)
@@ -843,7 +848,7 @@ def qk_norm_bwd(q, k, dyq, dyk, *, norm="l2", q_weight=None, k_weight=None, eps=
     if out is not None:
         _on_gpu(q, dwq, dwk, ws)
     L_ = _lib.lib()
-    ctx, handle = _on(dev, stream)
+    ctx, handle = _on(dev, stream, q, k, q_weight, k_weight, inv_freq, pos, dyq, dyk, dq, dk, dwq, dwk, ws)
     with ctx:
         if out is None:
             dq, dk = _packed(q), _packed(k)

@@ -348,7 +348,8 @@ def test_gdn_streams_graph_and_repeat():
 
 
 def test_stream_of_the_tensors_device():
-    """Two streams at once, each on slots of its own in one pool."""
+    """Two streams at once, each on slots of its own in one pool; the bounds and slots are
+    let go of right after the call and their memory taken again."""
     cu, T = ref.sequences([70, 3])
     print("[gdn ragged] two streams", flush=True)
     args = gdn_inputs(T, 1, 2, 128, 64, 4, seed=22)
@@ -357,7 +358,9 @@ def test_stream_of_the_tensors_device():
     torch.cuda.synchronize()
     outs = [sf.gdn_ragged_fwd(*args, i32(cu), i32(sl), max_len=70, stream=st)
             for sl, st in zip(([0, 3], [2, 1]), streams)]
+    again = [i32([7, 7, 7]) for _ in range(64)] + [i32([9, 9]) for _ in range(64)]
     torch.cuda.synchronize()
+    assert len(again) == 128
     for o, w in zip(outs, want):
         close("o", o, w[0], DELTA)
     close("state", args[5][[0, 3]], want[0][2][[0, 3]], DELTA)

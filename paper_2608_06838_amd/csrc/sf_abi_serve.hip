@@ -221,12 +221,13 @@ struct Heads {
     int H;
     const char *name;
 };
-bool side_by_side(const Heads &a, const Heads &b, int D, size_t e) {
-    if (a.t.b != b.t.b || a.t.l != b.t.l) return false;
-    if ((uintptr_t)a.p > (uintptr_t)b.p) return side_by_side(b, a, D, e);
+bool side_by_side(const Heads &a, const Heads &b, const sf_qk_shape &s, size_t e) {
+    if ((s.B > 1 && a.t.b != b.t.b) || (s.L > 1 && a.t.l != b.t.l)) return false;
+    if ((uintptr_t)a.p > (uintptr_t)b.p) return side_by_side(b, a, s, e);
     const uint64_t d = (uintptr_t)b.p - (uintptr_t)a.p;
-    const uint64_t ea = ((uint64_t)(a.H - 1) * a.t.h + D) * e, eb = ((uint64_t)(b.H - 1) * b.t.h + D) * e;
-    return d >= ea && d + eb <= (uint64_t)a.t.l * e;
+    const uint64_t ea = ((uint64_t)(a.H - 1) * a.t.h + s.D) * e, eb = ((uint64_t)(b.H - 1) * b.t.h + s.D) * e;
+    // b's heads follow a's, and the next row of either, by token or by batch, follows both
+    return d >= ea && non_overlapping({{s.B, a.t.b}, {s.L, a.t.l}}, (int64_t)((d + eb + e - 1) / e));
 }
 sf_status check_qk_alias(const sf_qk_shape &s, const std::vector<Heads> &ins, const std::vector<Heads> &outs,
                          std::vector<Range> in, const std::vector<Range> &out) {
@@ -234,7 +235,7 @@ sf_status check_qk_alias(const sf_qk_shape &s, const std::vector<Heads> &ins, co
     auto range = [&](const Heads &h) {
         return strided(h.p, {{s.B, h.t.b}, {s.L, h.t.l}, {h.H, h.t.h}}, s.D, e, h.name);
     };
-    auto clash = [&](const Heads &a, const Heads &b) { return overlap(range(a), range(b)) && !side_by_side(a, b, s.D, e); };
+    auto clash = [&](const Heads &a, const Heads &b) { return overlap(range(a), range(b)) && !side_by_side(a, b, s, e); };
     for (size_t i = 0; i < outs.size(); ++i) {
         for (auto &x : ins)
             if (clash(outs[i], x)) return fail(SF_E_ALIAS, "output %s overlaps input %s", outs[i].name, x.name);

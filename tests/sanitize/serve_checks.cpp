@@ -193,6 +193,12 @@ int main() {
             c.s.Hq = 2; c.s.yq = {10 * 512, 512, 128})
     REFUSED(Qk, fwd, SF_E_ALIAS, c.s.yq = c.s.yk = wide; c.yk = (char *)c.yq + 4 * 128 * 2 - 16)
     REFUSED(Qk, fwd, SF_E_ALIAS, c.s.yq = c.s.yk = wide; c.yk = (char *)c.yq + 6 * 128 * 2 + 16)
+    // batches inside a token's row: its heads of all batches must stay clear of each other
+    REFUSED(Qk, fwd, SF_OK, c.s.B = 2; c.s.yq = c.s.yk = {1024, 4096, 128}; c.yk = (char *)c.yq + 4 * 128 * 2)
+    REFUSED(Qk, fwd, SF_E_ALIAS, c.s.B = 2; c.s.yq = c.s.yk = {768, 4096, 128}; c.yk = (char *)c.yq + 768 * 2)
+    REFUSED(Qk, fwd, SF_E_ALIAS, c.s.B = 2; c.s.L = 1; c.s.yq = c.s.yk = {768, 4096, 128}; c.yk = (char *)c.yq + 768 * 2)
+    // a single token's stride means nothing
+    REFUSED(Qk, fwd, SF_OK, c.s.B = 2; c.s.L = 1; c.s.yq = {1024, 0, 128}; c.s.yk = {1024, 8, 128}; c.yk = (char *)c.yq + 512 * 2)
     rec = {};
 
     // ---- accepted calls

@@ -80,9 +80,36 @@ __device__ __forceinline__ void split3(const f32x4 &a, const f32x4 &b, bf16x8 &h
     split3(x, hi, mid, lo);
 }
 
-// e^-104 is below the smallest fp32: a gate of -inf (forget everything) becomes one
-// whose running sum stays finite (and NaN stays NaN)
-__device__ __forceinline__ float gate_log2(float g) { return (g < -104.f ? -104.f : g) * LOG2E; }
+// A chunk's running sum of gates (in powers of two) is formed in 64 bits and kept as a
+// pair of floats: a decay is the difference of two sums, and behind strong gates both are
+// large (some thousands where documents reset the state), so that sums in 32 bits would
+// leave a weak gate's decay with the large sums' error: 1e-4 of the state behind four
+// resets, 1e-6 with gates near -0.1; the pair leaves 1e-7.  e^-104 is below the smallest
+// fp32: a gate of -inf (forget everything) becomes one whose sum stays finite (and NaN
+// stays NaN).
+__device__ __forceinline__ double gate_log2(float g) { return (double)(g < -104.f ? -104.f : g) * 1.4426950408889634; }
+template <int CTRL, int ROWS = 0xf>
+__device__ __forceinline__ double dpp_or0(double x) {
+    const uint64_t u = __builtin_bit_cast(uint64_t, x);
+    const unsigned lo = (unsigned)__builtin_amdgcn_update_dpp(0, (int)(unsigned)u, CTRL, ROWS, 0xf, true);
+    const unsigned hi = (unsigned)__builtin_amdgcn_update_dpp(0, (int)(unsigned)(u >> 32), CTRL, ROWS, 0xf, true);
+    return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+__device__ __forceinline__ double wave_scan_dpp(double x) {  // as for floats
+    x += dpp_or0<0x111>(x);
+    x += dpp_or0<0x112>(x);
+    x += dpp_or0<0x114>(x);
+    x += dpp_or0<0x118>(x);
+    x += dpp_or0<0x142, 0xa>(x);
+    x += dpp_or0<0x143, 0xc>(x);
+    return x;
+}
+__device__ __forceinline__ double lane_value(double x, int l) {
+    const uint64_t u = __builtin_bit_cast(uint64_t, x);
+    const unsigned lo = (unsigned)__builtin_amdgcn_readlane((int)(unsigned)u, l);
+    const unsigned hi = (unsigned)__builtin_amdgcn_readlane((int)(unsigned)(u >> 32), l);
+    return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
 
 // Rows [0, 64) of a chunk tile of D channels, in 16-byte blocks over NT threads, rows
 // from m on the last one again; to LDS with pitch LD, rows of bit 3 swizzled by SW channels (see
@@ -179,7 +206,7 @@ __global__ void __launch_bounds__(256, 4) k_rag_prep(GdnRaggedArgs a) {
     __bf16 *const sK = reinterpret_cast<__bf16 *>(mem);
     float *const sA = reinterpret_cast<float *>(mem);
     __shared__ __attribute__((aligned(16))) float sT[64 * LA];
-    __shared__ __attribute__((aligned(16))) float sb[64], sbeta[64];
+    __shared__ __attribute__((aligned(16))) float sb[64], sbl[64], sbeta[64];  // sums (high, low), beta
     const int tid = threadIdx.x, lane = tid & 63, q4 = lane >> 4, n16 = lane & 15;
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
     if (blockIdx.x == 0) {
@@ -231,17 +258,19 @@ __global__ void __launch_bounds__(256, 4) k_rag_prep(GdnRaggedArgs a) {
         if (w == 0) {
             const bool in = lane < m;
             const int64_t go = (row0 + lane) * a.sg_t + hv * a.sg_h;
-            const float b = wave_scan_dpp(in ? gate_log2(a.g[go]) : 0.f), be = in ? a.beta[go] : 0.f;
-            sb[lane] = b;
+            const double b = wave_scan_dpp(in ? gate_log2(a.g[go]) : 0.0);
+            const float be = in ? a.beta[go] : 0.f, hi = (float)b;
+            sb[lane] = hi;
+            sbl[lane] = (float)(b - hi);
             sbeta[lane] = be;
             float *const gates = reinterpret_cast<float *>(a.ws + (id * a.Hv + hv) * (int64_t)RAG_SYS + RAG_GATES) + lane;
-            gates[0] = fexp2(b);
-            gates[64] = fexp2(lane_value(b, 63) - b);
+            gates[0] = fexp2(hi);
+            gates[64] = fexp2((float)(lane_value(b, 63) - b));
             gates[128] = be;
         }
         __syncthreads();
         __bf16 *const sys = reinterpret_cast<__bf16 *>(a.ws + (id * a.Hv + hv) * (int64_t)RAG_SYS);
-        const float bt = sb[tok], be = sbeta[tok];
+        const float bt = sb[tok], btl = sbl[tok], be = sbeta[tok];
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks) {
             if (ks > (w >> 1)) continue;
@@ -249,7 +278,7 @@ __global__ void __launch_bounds__(256, 4) k_rag_prep(GdnRaggedArgs a) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const int s = 32 * ks + 8 * q4 + j;
-                const float d = fexp2(bt - sb[s]);
+                const float d = fexp2((bt - sb[s]) + (btl - sbl[s]));
                 av[j] = s < tok ? be * kk[2 * ks + (j >> 2)][j & 3] * d : 0.f;
                 pv[j] = s <= tok ? qk[2 * ks + (j >> 2)][j & 3] * d : 0.f;
             }

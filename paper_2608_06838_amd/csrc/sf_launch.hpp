@@ -161,10 +161,10 @@ struct GdnRaggedArgs {
 // 64 67 / 85): launches of at most TOK_FEW full waves a CU.
 constexpr int TOK_CL = 8, TOK_FEW = 2;
 inline int64_t gdn_token_waves(const GdnRaggedArgs &a, int cl = TOK_CL) { return (int64_t)a.r.N * a.Hv * (a.Dv / (4 * cl)); }
-// A chunk's triangular system, as operand fragments: T = (I + A)^-1 in three bf16
-// planes (exact), P in two, six fragments of 1 KB a plane, then the chunk's e^b,
-// e^(b_63 - b) and beta (sf_ragged_chunk.hip)
-constexpr int RAG_FRAGS = 6, RAG_TP = 3, RAG_PP = 2, RAG_SYS = ((RAG_TP + RAG_PP) * RAG_FRAGS + 1) * 1024;
+// A chunk's triangular system: T = (I + A)^-1 as operand fragments in three bf16 planes
+// (exact), six of 1 KB a plane, R = P T as it is in 12 tiles of 16 x 16, then the chunk's
+// e^b, e^(b_63 - b) and beta (sf_ragged_chunk.hip)
+constexpr int RAG_FRAGS = 6, RAG_TP = 3, RAG_R = RAG_TP * RAG_FRAGS * 1024, RAG_GATES = RAG_R + 12 * 1024, RAG_SYS = RAG_GATES + 1024;
 // Sequences up to so many tokens are taken token by token: a chunk costs the same
 // whatever its tokens, a token what the CUs' other waves leave it (20 heads of 128, us in
 // chunks / token by token: one sequence of 8 tokens 12.8 / 8.9, of 12 12.9 / 11.7, of 16
@@ -186,7 +186,7 @@ inline int64_t gdn_walk_groups(const GdnRaggedArgs &a) {
 // single column tiles, then their numbers, longest first
 inline size_t gdn_plan_at(const GdnRaggedArgs &a) { return (size_t)a.n_chunks * (size_t)a.Hv * RAG_SYS; }
 inline size_t gdn_chunk_ws_bytes(const GdnRaggedArgs &a) { return gdn_plan_at(a) + 4 * ((size_t)a.r.N + 2); }
-// T and P of every chunk and the plan; then the walk, with the other sequences' tokens
+// T and R of every chunk and the plan; then the walk, with the other sequences' tokens
 hipError_t launch_gdn_chunk_prep(const GdnRaggedArgs &a, hipStream_t s, hipEvent_t e0, hipEvent_t e1);
 hipError_t launch_gdn_chunk_walk(const GdnRaggedArgs &a, hipStream_t s, hipEvent_t e0, hipEvent_t e1);
 hipError_t launch_gdn_tokens(const GdnRaggedArgs &a, hipStream_t s, hipEvent_t e0, hipEvent_t e1);

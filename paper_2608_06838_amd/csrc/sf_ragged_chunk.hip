@@ -4,19 +4,21 @@
 // Chunk algebra (S the state entering the chunk, b_t the chunk's running sum of g,
 // rows past the sequence's end with beta = 0 and g = 0):
 //   A[t][s] = beta_t e^(b_t - b_s) k_t.k_s  (s < t),   T = (I + A)^-1
-//   P[t][s] = e^(b_t - b_s) q_t.k_s         (s <= t)
-//   U = T diag(beta) (V - diag(e^b) K S),   O = diag(e^b) Q S + P U
+//   P[t][s] = e^(b_t - b_s) q_t.k_s         (s <= t),  R = P T
+//   X = diag(beta) (V - diag(e^b) K S),   U = T X,   O = diag(e^b) Q S + R X  (P U = R X)
 //   S <- e^(b_63) S + K^T diag(e^(b_63 - b)) U
-// T and P need no state: k_rag_prep forms them for every chunk at once, and k_rag_walk
+// T and R need no state: k_rag_prep forms them for every chunk at once, and k_rag_walk
 // takes the chunks of one sequence and value head in order.
 //
 // The state leaves this call in fp32 and enters the next one, thousands of times in a
 // decoded sequence, so it is carried as precisely as the token-by-token kernel carries
-// it: every product that reaches it runs on bf16 MFMA with its fp32 operands cut into
-// three bf16 pieces of eight bits (exact: 24 bits), keys entering as the bf16 they are.
-// Of the nine products of T's and X's pieces the three below 2^-24 are left out.  U and P
-// enter the output, which is rounded to bf16, as pairs (2^-17).  Against fp32 matrix
-// instructions that is 3 to 6 instructions at 16 times the rate.
+// it, and outputs are as exact before their rounding: every product of the walk runs on
+// bf16 MFMA with its fp32 operands cut into three bf16 pieces of eight bits (exact: 24
+// bits), keys and queries entering as the bf16 they are.  Of the nine products of two
+// operands' pieces the three below 2^-24 are left out.  Against fp32 matrix instructions
+// that is 3 to 6 instructions at 16 times the rate.  Outputs take X, whose pieces U needs
+// anyway: U's own would be a second set through LDS (8259 packed tokens of 20 heads: 229 us
+// that way, 224 this).
 //
 // State columns never mix, so a workgroup of the walk owns 16 NC of them.  Its four
 // waves share each chunk's chain of products by rows: wave w forms the rows of its 16
@@ -135,10 +137,10 @@ struct RowTile {
     }
 };
 
-constexpr int RAG_GATES = (RAG_TP + RAG_PP) * RAG_FRAGS * 1024;  // where a system's gates begin
-
 // fragment (tt, ks) of a lower triangle: tiles 0, 1 have columns 0..31 only
 __device__ __forceinline__ constexpr int tri_frag(int tt, int ks) { return tt < 2 ? tt : 2 + 2 * (tt - 2) + ks; }
+// tile (tt, c) of such a triangle, two to a fragment
+__device__ __forceinline__ constexpr int tri_tile16(int tt, int c) { return 2 * tri_frag(tt, c >> 1) + (c & 1); }
 
 // The sequences that are taken in chunks, longest first: the walk's time is that of
 // its longest sequence once the others no longer fill the chip, so that one starts
@@ -196,7 +198,7 @@ __device__ __forceinline__ void make_plan(const GdnRaggedArgs &a, int *at, int t
         if (const int64_t n = length(i)) a.plan[2 + atomicAdd(&at[plan_bucket(n)], 1)] = i;
 }
 
-// ---------------------------------------------------------------- T and P of a chunk
+// ---------------------------------------------------------------- T and R of a chunk
 template <int DK>
 __global__ void __launch_bounds__(256, 4) k_rag_prep(GdnRaggedArgs a) {
     constexpr int NT = 256, LD = DK + 16, SW = swx<__bf16, DK>(), LA = 68;
@@ -252,8 +254,10 @@ __global__ void __launch_bounds__(256, 4) k_rag_prep(GdnRaggedArgs a) {
             mma(qk[st], kf, qt[ks]);
         }
     }
-    const int tok = 16 * w + n16;
     for (int hv = hk * group; hv < (hk + 1) * group; ++hv) {
+        int ln = lane;
+        asm volatile("" : "+v"(ln));  // addresses are formed for each head, not held in registers all the while
+        const int lane = ln, q4 = lane >> 4, n16 = lane & 15, tok = 16 * w + n16;
         __syncthreads();  // the last head is done with the gates, with A and T (the first: all with K)
         if (w == 0) {
             const bool in = lane < m;
@@ -271,25 +275,21 @@ __global__ void __launch_bounds__(256, 4) k_rag_prep(GdnRaggedArgs a) {
         __syncthreads();
         __bf16 *const sys = reinterpret_cast<__bf16 *>(a.ws + (id * a.Hv + hv) * (int64_t)RAG_SYS);
         const float bt = sb[tok], btl = sbl[tok], be = sbeta[tok];
+        float pv[2][8] = {};  // P's row tok, columns 32 ks + 8 q4 ..
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks) {
             if (ks > (w >> 1)) continue;
-            float av[8], pv[8];
+            float av[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const int s = 32 * ks + 8 * q4 + j;
-                const float d = fexp2((bt - sb[s]) + (btl - sbl[s]));
+                const float d = fexp2((bt - sb[s]) + (btl - sbl[s]));  // e^(b_tok - b_s)
                 av[j] = s < tok ? be * kk[2 * ks + (j >> 2)][j & 3] * d : 0.f;
-                pv[j] = s <= tok ? qk[2 * ks + (j >> 2)][j & 3] * d : 0.f;
+                pv[ks][j] = s <= tok ? qk[2 * ks + (j >> 2)][j & 3] * d : 0.f;
             }
             float *p = &sA[tok * LA + 32 * ks + 8 * q4];
             *reinterpret_cast<f32x4 *>(p) = f32x4{av[0], av[1], av[2], av[3]};
             *reinterpret_cast<f32x4 *>(p + 4) = f32x4{av[4], av[5], av[6], av[7]};
-            bf16x8 hi, lo;
-            split8<__bf16, true>(pv, hi, lo);
-            __bf16 *out = sys + (RAG_TP * RAG_FRAGS + tri_frag(w, ks)) * 512 + 8 * lane;
-            *reinterpret_cast<bf16x8 *>(out) = hi;
-            *reinterpret_cast<bf16x8 *>(out + RAG_FRAGS * 512) = lo;
         }
         __syncthreads();
         // Diagonal blocks by forward substitution, a column a thread: x_r = [r == c] -
@@ -347,7 +347,29 @@ __global__ void __launch_bounds__(256, 4) k_rag_prep(GdnRaggedArgs a) {
             }
         }
         __syncthreads();
-        // fragments of tile w: rows 16 w + n16, columns 32 ks + 8 q4 ..
+        // Rows 16 w .. of R = P T in fp32 MFMA, as R^T = T^T P^T: lane (q4, n16) gets four
+        // columns of row 16 w + n16.  P lies in the wave's own rows of sA (A has had its last
+        // read).  The wave with the most blocks here had the fewest above.
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks) {
+            if (ks > (w >> 1)) continue;
+            float *p = &sA[tok * LA + 32 * ks + 8 * q4];
+            *reinterpret_cast<f32x4 *>(p) = f32x4{pv[ks][0], pv[ks][1], pv[ks][2], pv[ks][3]};
+            *reinterpret_cast<f32x4 *>(p + 4) = f32x4{pv[ks][4], pv[ks][5], pv[ks][6], pv[ks][7]};
+        }
+        f32x4 acc[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            acc[k] = f32x4{0.f, 0.f, 0.f, 0.f};
+            if (k > w) continue;
+            const f32x4 pk = *reinterpret_cast<const f32x4 *>(&sA[tok * LA + 16 * k + 4 * q4]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+#pragma unroll
+                for (int c = 0; c <= k; ++c)
+                    acc[c] = __builtin_amdgcn_mfma_f32_16x16x4f32(sT[(16 * k + 4 * q4 + e) * LA + 16 * c + n16], pk[e], acc[c], 0, 0, 0);
+        }
+        // T's fragments of tile w: rows 16 w + n16, columns 32 ks + 8 q4 ..
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks) {
             if (ks > (w >> 1)) continue;
@@ -358,26 +380,31 @@ __global__ void __launch_bounds__(256, 4) k_rag_prep(GdnRaggedArgs a) {
             for (int pl = 0; pl < RAG_TP; ++pl)
                 *reinterpret_cast<bf16x8 *>(sys + (pl * RAG_FRAGS + tri_frag(w, ks)) * 512 + 8 * lane) = f[pl];
         }
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+            if (c <= (w | 1))
+                *reinterpret_cast<f32x4 *>(reinterpret_cast<char *>(sys) + RAG_R + tri_tile16(w, c) * 1024 + 16 * lane) = acc[c];
     }
 }
 
 // ----------------------------------------------------------------------- the walk
 // Per chunk, with barriers between the phases:
 //   S's pieces to LDS | K S, Q S of the wave's tokens, X = beta (V - e^b K S) to LDS |
-//   U = T X, to LDS in three pieces times e^(b_63 - b) and as a pair | O, S
-// K, Q, T and P are needed by one wave each, in fragment order: they come from memory
-// into registers a chunk ahead and pass LDS only where K is read transposed.
+//   U = T X, to LDS in three pieces times e^(b_63 - b) | O, S
+// K, Q, T and R are needed by one wave each, in fragment order: they come from memory
+// into registers a chunk ahead and pass LDS only where K is read transposed.  R comes as
+// it is, 12 KB instead of 18, and is cut beside the first products.
 // Everything a chunk loads is waited for at one place, before the last chunk's outputs
 // are stored: loads and stores share a counter (see vm_wait_all).
 
 // LDS of a walk workgroup.  NC >= 2: K's tile and U's pieces lie where S's pieces were,
-// so that two workgroups share a CU; one barrier more keeps the next chunk's S behind
+// which keeps the whole within 64 KB; one barrier more keeps the next chunk's S behind
 // their last reads.
 template <int DK, int NC>
 struct WalkLds {
     static constexpr int LD = DK + 16, CW = 16 * NC, LS = DK + 16, LT = 64 + 16;
     static constexpr bool ALIAS = NC >= 2;
-    static constexpr int NSP = 3 * CW * LS, NX = 3 * CW * LT, NU = 5 * CW * LT, NKT = 64 * LD;
+    static constexpr int NSP = 3 * CW * LS, NX = 3 * CW * LT, NU = 3 * CW * LT, NKT = 64 * LD;
     static constexpr int SIZE = NX + (ALIAS ? (NSP > NU + NKT ? NSP : NU + NKT) : NSP + NU + NKT);
 };
 
@@ -390,7 +417,9 @@ __device__ __forceinline__ void rag_walk(const GdnRaggedArgs &a, __bf16 *mem, in
     typedef WalkLds<DK, NC> L;
     constexpr bool ALIAS = L::ALIAS;
     __bf16 *const sX = mem, *const sS = mem + L::NX, *const sU = ALIAS ? sS : sS + L::NSP, *const sK = sU + L::NU;
-    const int tid = threadIdx.x, lane = tid & 63, q4 = lane >> 4, n16 = lane & 15;
+    int tid = threadIdx.x;
+    asm volatile("" : "+v"(tid));  // what follows from the lane is formed for each item, not held in registers between them
+    const int lane = tid & 63, q4 = lane >> 4, n16 = lane & 15;
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const Seq s = seq_of(a.r, i);
     const int64_t n = s.end - s.begin;
@@ -414,11 +443,12 @@ __device__ __forceinline__ void rag_walk(const GdnRaggedArgs &a, __bf16 *mem, in
 #pragma unroll
             for (int r = 0; r < 4; ++r) S[t][c][r] = fresh ? 0.f : st[(int64_t)(16 * t + r) * a.Dv + 16 * c];
 
-    bf16x8 kf[NK], qf[NK], t0[RAG_TP], t1[RAG_TP], p0[RAG_PP], p1[RAG_PP];
+    bf16x8 kf[NK], qf[NK], t0[RAG_TP], t1[RAG_TP];
+    f32x4 rf[2][2];  // R's row tok, columns 32 ks + 8 q4 ..
     unsigned short vf[NC][4];
     f32x4 eb, ee, be;  // of the wave's rows 16 w + 4 q4 + r
     float et, gam;     // e^b of token 16 w + n16, of the chunk
-    const bool two = w >= 2;  // the wave's tile of T and P has a second k-step
+    const bool two = w >= 2;  // the wave's tile of T and R has a second k-step
     // rows past the sequence's end stand for its last one: their beta is 0, so they
     // change nothing
     auto last_row = [&](int64_t c) { return n - c < 64 ? (int)(n - c) - 1 : 63; };
@@ -451,14 +481,14 @@ __device__ __forceinline__ void rag_walk(const GdnRaggedArgs &a, __bf16 *mem, in
                 t1[pl] = *reinterpret_cast<const bf16x8 *>(p + f0 + (pl * RAG_FRAGS + 1) * 1024 + l16);
         }
     };
-    auto fetch_p = [&](const char *p) {
-        p += RAG_TP * RAG_FRAGS * 1024;
+    const uint32_t r16 = 1024 * (q4 >> 1) + 512 * (q4 & 1) + 16 * n16;
+    auto fetch_r = [&](const char *p) {
+        p += RAG_R + 2 * f0;
 #pragma unroll
-        for (int pl = 0; pl < RAG_PP; ++pl) p0[pl] = *reinterpret_cast<const bf16x8 *>(p + f0 + pl * RAG_FRAGS * 1024 + l16);
+        for (int m = 0; m < 2; ++m) rf[0][m] = *reinterpret_cast<const f32x4 *>(p + r16 + 256 * m);
         if (two) {
 #pragma unroll
-            for (int pl = 0; pl < RAG_PP; ++pl)
-                p1[pl] = *reinterpret_cast<const bf16x8 *>(p + f0 + (pl * RAG_FRAGS + 1) * 1024 + l16);
+            for (int m = 0; m < 2; ++m) rf[1][m] = *reinterpret_cast<const f32x4 *>(p + 2048 + r16 + 256 * m);
         }
     };
     auto fetch_gates = [&](const char *p) {
@@ -472,12 +502,11 @@ __device__ __forceinline__ void rag_walk(const GdnRaggedArgs &a, __bf16 *mem, in
     const bf16x8 zero8 = __builtin_bit_cast(bf16x8, u32x4{0u, 0u, 0u, 0u});
 #pragma unroll
     for (int pl = 0; pl < RAG_TP; ++pl) t1[pl] = zero8;
-#pragma unroll
-    for (int pl = 0; pl < RAG_PP; ++pl) p1[pl] = zero8;
+    rf[1][0] = rf[1][1] = f32x4{0.f, 0.f, 0.f, 0.f};
     fetch_k(0);
     fetch_qv(0);
     fetch_t(sys);
-    fetch_p(sys);
+    fetch_r(sys);
     fetch_gates(sys);
     const LaneOff tr = tr_off<__bf16, L::LD, SW>(lane);
     bf16x4 out[NC];
@@ -512,6 +541,7 @@ __device__ __forceinline__ void rag_walk(const GdnRaggedArgs &a, __bf16 *mem, in
         // Operand fragments are read a step ahead of their products, and the fences keep it
         // so: left alone, the compiler may read each pair just before its use, and then
         // every two matrix instructions wait for LDS.
+        bf16x8 rp[2][3];     // R's pieces
         f32x4 X[NC], Y[NC];  // K S (rows: tokens 16 w + 4 q4 + r), (Q S)^T (columns: tokens 16 w + n16)
         {
             bf16x8 f[2][NK];
@@ -533,6 +563,8 @@ __device__ __forceinline__ void rag_walk(const GdnRaggedArgs &a, __bf16 *mem, in
                     mma(X[x], kf[ks], f[step & 1][ks]);
                     mma(Y[x], f[step & 1][ks], qf[ks]);
                 }
+                if (step == 0) split3(rf[0][0], rf[0][1], rp[0][0], rp[0][1], rp[0][2]);
+                if (step == 1) split3(rf[1][0], rf[1][1], rp[1][0], rp[1][1], rp[1][2]);
                 sched_fence();
             }
         }
@@ -563,6 +595,22 @@ __device__ __forceinline__ void rag_walk(const GdnRaggedArgs &a, __bf16 *mem, in
         for (int ks = 0; ks < NK; ++ks)
             *reinterpret_cast<bf16x8 *>(sK + tok * L::LD + swz_col(tok, 32 * ks + 8 * q4, SW)) = kf[ks];
         if (more) fetch_k(c + 64);
+        // O^T = e^b (Q S)^T + X^T R^T; the last tile's while the next phase's operands come from LDS
+        auto out_products = [&](int x) {
+            Y[x] *= et;
+            f32x4 Y1 = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int ks = 0; ks < 2; ++ks) {
+                if (ks == 1 && !two) continue;
+                mma(Y1, xf[x][0][ks], rp[ks][2]);
+                mma(Y[x], xf[x][1][ks], rp[ks][1]);
+                mma(Y1, xf[x][2][ks], rp[ks][0]);
+                mma(Y[x], xf[x][1][ks], rp[ks][0]);
+                mma(Y1, xf[x][0][ks], rp[ks][1]);
+                mma(Y[x], xf[x][0][ks], rp[ks][0]);
+            }
+            Y[x] += Y1;
+        };
         f32x4 U[NC];
 #pragma unroll
         for (int x = 0; x < NC; ++x) {
@@ -580,16 +628,12 @@ __device__ __forceinline__ void rag_walk(const GdnRaggedArgs &a, __bf16 *mem, in
                 mma(U[x], t[0], xf[x][0][ks]);
             }
             U[x] += U1;
-            bf16x4 f[5];
+            if (x + 1 < NC) out_products(x);
+            bf16x4 f[3];
             const f32x4 ue = U[x] * ee;
             split3(ue, f[0], f[1], f[2]);
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                f[3][r] = (__bf16)U[x][r];
-                f[4][r] = (__bf16)(U[x][r] - (float)f[3][r]);
-            }
-#pragma unroll
-            for (int p = 0; p < 5; ++p)
+            for (int p = 0; p < 3; ++p)
                 *reinterpret_cast<bf16x4 *>(sU + (p * CW + 16 * x + n16) * L::LT + 16 * w + 4 * q4) = f[p];
         }
         if (more) fetch_t(next);
@@ -597,41 +641,21 @@ __device__ __forceinline__ void rag_walk(const GdnRaggedArgs &a, __bf16 *mem, in
         auto u_piece = [&](int x, int p, int ks) {
             return *reinterpret_cast<const bf16x8 *>(sU + (p * CW + 16 * x + n16) * L::LT + 32 * ks + 8 * q4);
         };
-        bf16x8 po[2][2][2], uf[2][3][2], kt[NS][2];  // U's pair, its pieces, K^T
-        auto read_pair = [&](int x) {
-#pragma unroll
-            for (int p = 0; p < 2; ++p)
-#pragma unroll
-                for (int ks = 0; ks < 2; ++ks) po[x & 1][p][ks] = u_piece(x, 3 + p, ks);
-        };
+        bf16x8 uf[2][3][2], kt[NS][2];  // U's pieces, K^T
         auto read_pieces = [&](int x) {
 #pragma unroll
             for (int p = 0; p < 3; ++p)
 #pragma unroll
                 for (int ks = 0; ks < 2; ++ks) uf[x & 1][p][ks] = u_piece(x, p, ks);
         };
-        read_pair(0);
+        read_pieces(0);
+        sched_fence();
+        out_products(NC - 1);
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
             for (int t = 0; t < NS; ++t) kt[t][ks] = ldfragTR<__bf16, L::LD, SW>(sK, tr, 32 * ks, 16 * (NS * w + t));
-        // O^T = e^b (Q S)^T + U^T P^T
-#pragma unroll
-        for (int x = 0; x < NC; ++x) {
-            if (x + 1 < NC) read_pair(x + 1);
-            else read_pieces(0);
-            sched_fence();
-            Y[x] *= et;
-#pragma unroll
-            for (int ks = 0; ks < 2; ++ks) {
-                if (ks == 1 && !two) continue;
-                mma(Y[x], po[x & 1][0][ks], ks ? p1[1] : p0[1]);
-                mma(Y[x], po[x & 1][1][ks], ks ? p1[0] : p0[0]);
-                mma(Y[x], po[x & 1][0][ks], ks ? p1[0] : p0[0]);
-            }
-            sched_fence();
-        }
-        if (more) fetch_p(next);
+        if (more) fetch_r(next);
         // S = e^(b_63) S + K^T e^(b_63 - b) U
 #pragma unroll
         for (int x = 0; x < NC; ++x) {

@@ -286,15 +286,15 @@ __global__ void __launch_bounds__(QK_NT, qk_resident(BWD, WGT)) k_qk(QkArgs a) {
                         }
                     }
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        o[e] = dz[e] * (scale * wt[e]);
-                        dot = fmaf(o[e], f[e], dot);
-                    }
-                    dot = row_sum<LPR>(dot);
-                    const float c = a.norm == SF_NORM_NONE ? 0.f : a.norm == SF_NORM_L2 ? 1.f : 1.f / (float)a.D;
-                    const float m = c * rn * rn * dot;
+                    for (int e = 0; e < 8; ++e) o[e] = dz[e] * (scale * wt[e]);
+                    if (a.norm != SF_NORM_NONE) {  // without a norm x has no part in dx, whatever it holds
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) o[e] = rn * (o[e] - m * f[e]);
+                        for (int e = 0; e < 8; ++e) dot = fmaf(o[e], f[e], dot);
+                        const float c = a.norm == SF_NORM_L2 ? 1.f : 1.f / (float)a.D;
+                        const float m = c * rn * rn * row_sum<LPR>(dot);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) o[e] = rn * (o[e] - m * f[e]);
+                    }
                 }
                 if (live && h < H) store8<T>(key ? yk + h * a.syk.h : yq + h * a.syq.h, o);
             }

@@ -158,15 +158,20 @@ __device__ __forceinline__ int partner_ch(const QkArgs &a, int j) {
     return 8 * (j < hp ? j + hp : j - hp);
 }
 
-// the partners of a piece: another lane's, or the neighbours
+// the partners of a piece: another lane's, or the neighbours; zero behind the rotated
+// channels, where an infinity times sin = 0 would be NaN
 template <typename T>
 __device__ __forceinline__ void partners(const QkArgs &a, const Turn &t, const Oct<T> &x, const float (&f)[8],
-                                         float (&p)[8]) {
+                                         float (&p)[8], int ch) {
     if (a.inter) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) p[e] = f[e ^ 1];
     } else {
         x.from(t.addr).f32(p);
+    }
+    if (a.R < a.D) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) p[e] = ch < a.R ? p[e] : 0.f;
     }
 }
 
@@ -259,7 +264,7 @@ __global__ void __launch_bounds__(QK_NT, qk_resident(BWD, WGT)) k_qk(QkArgs a) {
                     const float m = rn * scale;
                     if (a.R) {
                         float p[8];
-                        partners<T>(a, t, x[u], f, p);
+                        partners<T>(a, t, x[u], f, p, ch);
 #pragma unroll
                         for (int e = 0; e < 8; ++e) o[e] = m * fmaf(f[e], wt[e] * t.c[e], p[e] * (wp[e] * t.s[e]));
                     } else {
@@ -271,7 +276,7 @@ __global__ void __launch_bounds__(QK_NT, qk_resident(BWD, WGT)) k_qk(QkArgs a) {
                     d[u].f32(dz);
                     if (a.R) {  // the transposed turn: sin changes its sign
                         float p[8];
-                        partners<T>(a, t, d[u], dz, p);
+                        partners<T>(a, t, d[u], dz, p, ch);
 #pragma unroll
                         for (int e = 0; e < 8; ++e) dz[e] = fmaf(dz[e], t.c[e], -(p[e] * t.s[e]));
                     }

@@ -117,8 +117,12 @@ __device__ __forceinline__ void turn_at(Turn &t, const QkArgs &a, int ch, int64_
     if (ch >= a.R) return;
     auto sincos = [&](double f, float &sn, float &cs) {
         double rev = (double)p * f;  // revolutions
-        rev -= rint(rev);
-        sincospif((float)(2.0 * rev), &sn, &cs);
+        rev = 2.0 * (rev - rint(rev));
+        const float hi = (float)rev, lo = 3.14159265358979f * (float)(rev - hi);
+        float s0, c0;
+        sincospif(hi, &s0, &c0);
+        sn = fmaf(c0, lo, s0);  // what the float leaves of the angle, up to pi 2^-25, in first order
+        cs = fmaf(-s0, lo, c0);
     };
     if (a.inter) {
 #pragma unroll

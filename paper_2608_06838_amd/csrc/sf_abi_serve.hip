@@ -213,21 +213,38 @@ sf_status check_qk_turn(const sf_qk_shape &s, const double *inv_freq, const int6
                                                           : SF_OK;
 }
 
-// Heads of one tensor as its rows see them: two tensors whose rows lie side by side
-// in wider rows (slices of one projection) share memory spans and no element.
+// One tensor of heads.  Two whose spans overlap may still share no element: slices of one
+// projection, or of one buffer with the heads outermost.
 struct Heads {
     const void *p;
     sf_strides t;
     int H;
     const char *name;
 };
+// Whether some of the dims that both tensors step through alike (size and stride) leave,
+// taken away, spans that lie one behind the other and fit together into those dims' cells.
 bool side_by_side(const Heads &a, const Heads &b, const sf_qk_shape &s, size_t e) {
-    if ((s.B > 1 && a.t.b != b.t.b) || (s.L > 1 && a.t.l != b.t.l)) return false;
     if ((uintptr_t)a.p > (uintptr_t)b.p) return side_by_side(b, a, s, e);
     const uint64_t d = (uintptr_t)b.p - (uintptr_t)a.p;
-    const uint64_t ea = ((uint64_t)(a.H - 1) * a.t.h + s.D) * e, eb = ((uint64_t)(b.H - 1) * b.t.h + s.D) * e;
-    // b's heads follow a's, and the next row of either, by token or by batch, follows both
-    return d >= ea && non_overlapping({{s.B, a.t.b}, {s.L, a.t.l}}, (int64_t)((d + eb + e - 1) / e));
+    const int64_t E = (int64_t)e;
+    const Dim da[3] = {{s.B, a.t.b * E}, {s.L, a.t.l * E}, {a.H, a.t.h * E}};
+    const Dim db[3] = {{s.B, b.t.b * E}, {s.L, b.t.l * E}, {b.H, b.t.h * E}};
+    for (int outer = 1; outer < 8; ++outer) {
+        std::vector<Dim> cells;
+        uint64_t ea = (uint64_t)(s.D * E), eb = ea;
+        bool alike = true;
+        for (int i = 0; i < 3; ++i) {
+            if (outer >> i & 1) {
+                alike = alike && da[i].size == db[i].size && (da[i].size == 1 || da[i].stride == db[i].stride);
+                cells.push_back(da[i]);
+            } else {
+                ea += (uint64_t)((da[i].size - 1) * da[i].stride);
+                eb += (uint64_t)((db[i].size - 1) * db[i].stride);
+            }
+        }
+        if (alike && d >= ea && d + eb <= (uint64_t)INT64_MAX && non_overlapping(cells, (int64_t)(d + eb))) return true;
+    }
+    return false;
 }
 sf_status check_qk_alias(const sf_qk_shape &s, const std::vector<Heads> &ins, const std::vector<Heads> &outs,
                          std::vector<Range> in, const std::vector<Range> &out) {

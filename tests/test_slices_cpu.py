@@ -1,0 +1,25 @@
+"""Outputs of the norms of queries and keys that lie between each other in one buffer: the
+host's checks under sanitizers, against launch stubs."""
+import os
+import subprocess
+
+import pytest
+
+from test_serve_cpu import CSRC, FLAGS, HIPCC, ROOT
+
+
+@pytest.mark.skipif(not os.path.exists(HIPCC), reason="hipcc not available")
+def test_slices_under_sanitizers(tmp_path):
+    exe = str(tmp_path / "slice_checks")
+    san = os.path.join(ROOT, "tests", "sanitize")
+    cmd = [HIPCC, "-x", "hip", "--offload-arch=gfx950", "-O1", "-g", "-std=c++17", "-fno-omit-frame-pointer",
+           "-Xarch_host", "-fsanitize=address", "-Xarch_host", "-fsanitize=undefined",
+           "-Xarch_host", "-fno-sanitize-recover=undefined", *FLAGS, "-I", os.path.join(ROOT, "include"), "-I", CSRC,
+           "-I", san, os.path.join(CSRC, "sf_abi.hip"), os.path.join(CSRC, "sf_abi_serve.hip"),
+           *(os.path.join(san, f) for f in ("launch_stubs.cpp", "serve_stubs.cpp", "slice_checks.cpp")), "-o", exe]
+    res = subprocess.run(cmd, capture_output=True, text=True)
+    assert res.returncode == 0, res.stderr[-3000:]
+    res = subprocess.run([exe], capture_output=True, text=True, timeout=120, env={
+        **os.environ, "ASAN_OPTIONS": "detect_leaks=0:verify_asan_link_order=0", "UBSAN_OPTIONS": "print_stacktrace=1"})
+    assert res.returncode == 0 and "slice checks passed" in res.stdout, res.stdout + res.stderr
+    print(res.stdout)

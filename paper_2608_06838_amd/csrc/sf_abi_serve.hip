@@ -106,7 +106,6 @@ sf_status check_gdn(const sf_gdn_ragged_shape *s, const sf_ragged *b) {
     return check_out("o", {{b->T, s->so_t}, {s->Hv, s->so_h}}, s->Dv, e);
 }
 
-int64_t gdn_chunks(const sf_ragged &b) { return b.T / 64 + b.N; }
 sf::GdnRaggedArgs gdn_args(const sf_gdn_ragged_shape &s, const sf_ragged &b) {
     sf::GdnRaggedArgs a{};
     a.r = ragged_args(b);
@@ -125,12 +124,12 @@ sf::GdnRaggedArgs gdn_args(const sf_gdn_ragged_shape &s, const sf_ragged &b) {
     a.sg_t = s.sg_t;
     a.sg_h = s.sg_h;
     a.ss = s.ss;
-    a.n_chunks = gdn_chunks(b);
     // Long sequences are taken in chunks where the operands are bf16, the host knows of
     // such a sequence and 64 rows span less than 2 GiB (the walk's offsets inside a chunk
     // are 32 bits); fp32 operands go token by token.
     const int few = sf::gdn_long(a);
-    if (s.io_dtype == SF_BF16 && b.max_len > few && std::max(s.sq_t, s.sv_t) < (int64_t)1 << 23) a.longer = few;
+    if (s.io_dtype == SF_BF16 && std::min(b.max_len, b.T) > few && std::max(s.sq_t, s.sv_t) < (int64_t)1 << 23) a.longer = few;
+    sf::gdn_number(a);
     return a;
 }
 size_t gdn_ragged_ws_bytes(const sf_gdn_ragged_shape &s, const sf_ragged &b) {

@@ -150,7 +150,8 @@ struct GdnRaggedArgs {
     int32_t Hk, Hv, Dk, Dv, io, n_cu;
     int64_t sq_t, sq_h, sv_t, sv_h, so_t, so_h, sg_t, sg_h, ss;
     int32_t longer;    // sequences of more tokens are taken in chunks (0: none are)
-    int64_t n_chunks;  // upper bound of the chunks: T / 64 + N
+    int32_t sys_div, sys_add;  // see gdn_first_system
+    int64_t n_chunks;  // numbers of chunk systems
     char *ws;          // chunk systems: [n_chunks][Hv] of RAG_SYS bytes
     int32_t *plan;     // [2 + N], see gdn_plan_at
 };
@@ -171,7 +172,22 @@ constexpr int RAG_FRAGS = 6, RAG_TP = 3, RAG_R = RAG_TP * RAG_FRAGS * 1024, RAG_
 // 12.9 / 14.4; 64 sequences of 16 tokens 86 / 67, of 24 91 / 89, of 32 91 / 114; 256 of 24
 // with 40 heads 674 / 637, of 32 696 / 839).
 constexpr int RAG_LONG = 24, RAG_LONG_FEW = 12;
+static_assert(RAG_LONG < 32 && RAG_LONG_FEW < 32, "n / (longer + 1) >= ceil(n / 64) from longer + 1 tokens on");
 inline int gdn_long(const GdnRaggedArgs &a) { return gdn_token_waves(a) <= a.n_cu ? RAG_LONG_FEW : RAG_LONG; }
+// Chunk systems are numbered without a table: those of sequence i, if it is taken in chunks,
+// begin at cu[i] / sys_div + sys_add i.  Either 64 and 1, T / 64 + N numbers: a sequence
+// has room for its last, short chunk.  Or longer + 1 and 0, T / (longer + 1) numbers: one of n
+// tokens, n > longer, has n / (longer + 1) >= ceil(n / 64) of them, and short sequences,
+// however many, none.  The fewer are taken (gdn_number).
+__host__ __device__ inline int64_t gdn_first_system(const GdnRaggedArgs &a, int64_t begin, int64_t i) {
+    return (int64_t)((uint32_t)begin / (uint32_t)a.sys_div) + a.sys_add * i;  // rows fit 31 bits
+}
+inline void gdn_number(GdnRaggedArgs &a) {
+    const int64_t all = a.r.T / 64 + a.r.N, few = a.longer ? a.r.T / (a.longer + 1) : all;
+    a.sys_div = few < all ? a.longer + 1 : 64;
+    a.sys_add = few < all ? 0 : 1;
+    a.n_chunks = few < all ? few : all;
+}
 // items of the walk with nc 16-column tiles each, for n sequences: (sequence, value
 // head) pairs in eights, their column blocks
 __host__ __device__ inline int64_t gdn_walk_items(const GdnRaggedArgs &a, int64_t n, int nc) {

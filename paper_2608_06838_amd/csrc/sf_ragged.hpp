@@ -23,13 +23,13 @@ __device__ __forceinline__ Seq seq_of(const RaggedArgs &r, int i) {
 // at cu[i] / run + i, which leaves it room for its own ceil(n / run) runs (its last one
 // may be short, and one number may stay unused), so a launch of T / run + N numbers
 // needs neither the lengths on the host nor a table.
-// the last sequence i in [0, N) whose first run is <= id; 64 candidates a step
-__device__ __forceinline__ int find_seq(const RaggedArgs &r, int run, int64_t id) {
+// the last sequence i in [0, N) whose first run, cu[i] / run + add i, is <= id; 64 candidates a step
+__device__ __forceinline__ int find_seq(const RaggedArgs &r, int run, int64_t id, int add = 1) {
     const int lane = threadIdx.x & 63;
     int lo = 0, n = r.N;
     while (n > 1) {
         const int step = (n + 63) / 64, i = lo + lane * step;
-        const bool in = lane * step < n && clamp_row(r.cu[lane * step < n ? i : lo], r.T) / run + i <= id;
+        const bool in = lane * step < n && (int64_t)((uint32_t)clamp_row(r.cu[lane * step < n ? i : lo], r.T) / (uint32_t)run) + (int64_t)add * i <= id;
         const int m = __popcll(__ballot(in));
         const int at = m > 0 ? (m - 1) * step : 0;
         lo += at;
@@ -37,7 +37,7 @@ __device__ __forceinline__ int find_seq(const RaggedArgs &r, int run, int64_t id
     }
     return __builtin_amdgcn_readfirstlane(lo);
 }
-__device__ __forceinline__ int64_t first_run(const Seq &s, int run, int i) { return s.begin / run + i; }
+__device__ __forceinline__ int64_t first_run(const Seq &s, int run, int i) { return (uint32_t)s.begin / (uint32_t)run + (int64_t)i; }
 
 // Gated delta rule, token by token (S <- e^g S, u = beta (v - S^T k), S <- S + k u^T,
 // o = S^T q).  A single token reads and writes the whole state for 6 flops an

@@ -218,9 +218,9 @@ __global__ void __launch_bounds__(256, 4) k_rag_prep(GdnRaggedArgs a) {
     const unsigned block = blockIdx.x - 1;
     const int hk = block % a.Hk, group = a.Hv / a.Hk;
     const int64_t id = block / a.Hk;
-    const int i = find_seq(a.r, 64, id);
+    const int i = find_seq(a.r, a.sys_div, id, a.sys_add);
     const Seq sq = seq_of(a.r, i);
-    const int64_t c0 = (id - first_run(sq, 64, i)) * 64, n = sq.end - sq.begin;
+    const int64_t c0 = (id - gdn_first_system(a, sq.begin, i)) * 64, n = sq.end - sq.begin;
     if (c0 < 0 || c0 >= n || n <= a.longer || sq.slot < 0) return;
     const int m = n - c0 < 64 ? (int)(n - c0) : 64;
     const int64_t row0 = sq.begin + c0;
@@ -429,7 +429,7 @@ __device__ __forceinline__ void rag_walk(const GdnRaggedArgs &a, __bf16 *mem, in
     const char *const Q = (const char *)a.q + 2 * (s.begin * a.sq_t + hk * a.sq_h);
     const char *const V = (const char *)a.v + 2 * (s.begin * a.sv_t + h * a.sv_h + cb * CW);
     __bf16 *const O = (__bf16 *)a.o + (s.begin + tok) * a.so_t + h * a.so_h + cb * CW + 4 * q4;
-    const char *const sys = a.ws + (first_run(s, 64, i) * a.Hv + h) * (int64_t)RAG_SYS;
+    const char *const sys = a.ws + (gdn_first_system(a, s.begin, i) * a.Hv + h) * (int64_t)RAG_SYS;
     const int64_t sys_step = (int64_t)a.Hv * RAG_SYS;
     float *const st = a.state + s.slot * a.ss + (int64_t)h * DK * a.Dv + (int64_t)(16 * NS * w + 4 * q4) * a.Dv + cb * CW + n16;
 

@@ -634,9 +634,10 @@ def _ragged(T, state, cu_seqlens, slots, fresh, max_len):
     if fresh is not None and (tuple(fresh.shape) != (N,) or fresh.dtype not in (torch.uint8, torch.bool)
                               or not fresh.is_contiguous()):
         raise ValueError(f"fresh must be a contiguous uint8 or bool tensor of {N} entries")
-    return _lib.SfRagged(N, N if state is None else state.shape[0], T,
-                         max(T - N + 1, 1) if max_len is None else int(max_len), cu_seqlens.data_ptr(), _addr(slots),
-                         _addr(fresh))
+    if max_len is None:  # with fewer tokens than sequences some are empty: how many, only the device knows
+        max_len = T if T < N else T - N + 1
+    return _lib.SfRagged(N, N if state is None else state.shape[0], T, int(max_len), cu_seqlens.data_ptr(),
+                         _addr(slots), _addr(fresh))
 
 
 def _gdn_ragged_args(q, k, v, g, beta, state, cu_seqlens, slots, fresh, max_len, o):
@@ -686,7 +687,9 @@ def gdn_ragged_fwd(q, k, v, g, beta, state, cu_seqlens, slots=None, *, fresh=Non
     last token.  Two sequences with tokens must not share a slot.  Rows of no sequence
     are left as they were in out=(o, workspace), and undefined in an o allocated here.
     max_len: the longest sequence if the host knows it (None: taken for N - 1 sequences
-    of one token and one with the rest); it steers the launch, not the result."""
+    of one token and one with the rest, or, with fewer tokens than sequences, for one with
+    all of them); it steers the launch, not the result.  Give it for a batch padded with
+    empty sequences: taken for short, a prompt runs token by token."""
     o, ws = (None, None) if out is None else out
     dev, sh, b = _gdn_ragged_args(q, k, v, g, beta, state, cu_seqlens, slots, fresh, max_len, o)
     if ws is not None:

@@ -17,7 +17,7 @@ pytestmark = pytest.mark.gpu
 def batches():
     rng = np.random.RandomState(9)
     yield "one prompt among single tokens", [1] * 150 + [333] + [1] * 100, 333
-    yield "one prompt among empty sequences", [0] * 200 + [300] + [0] * 200, 300
+    yield "one prompt among empty sequences", [0] * 200 + [300] + [0] * 200, None
     lens = [1] * 200 + [13, 25, 64, 65, 128, 129, 24, 12, 26] + [0] * 60
     rng.shuffle(lens)
     yield "lengths at every line", [int(x) for x in lens], 129

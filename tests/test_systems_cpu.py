@@ -1,9 +1,12 @@
 """Chunk systems of the ragged delta rule: how they are numbered, what workspace they
-take."""
+take, and the length a call without max_len assumes."""
 import os
 import subprocess
 
 import pytest
+import torch
+
+import paper_2608_06838_amd as sf
 
 from test_serve_cpu import CSRC, FLAGS, HIPCC, ROOT
 
@@ -22,3 +25,12 @@ def test_numbering_under_sanitizers(tmp_path):
     res = subprocess.run([exe], capture_output=True, text=True, timeout=120, env={
         **os.environ, "ASAN_OPTIONS": "detect_leaks=0:verify_asan_link_order=0", "UBSAN_OPTIONS": "print_stacktrace=1"})
     assert res.returncode == 0 and "system checks passed" in res.stdout, (res.stdout + res.stderr)[-3000:]
+
+
+@pytest.mark.parametrize("T,N,want", [(256, 256, 1), (2111, 64, 2048), (1000, 1024, 1000), (0, 3, 0), (5, 1, 5)])
+def test_length_without_a_hint(T, N, want):
+    """One token each but for one sequence; fewer tokens than sequences say nothing: any
+    one of them may have all."""
+    state, cu = torch.zeros(N, 1, 64, 64), torch.zeros(N + 1, dtype=torch.int32)
+    assert sf._ragged(T, state, cu, None, None, None).max_len == want
+    assert sf._ragged(T, state, cu, None, None, 7).max_len == 7

@@ -640,6 +640,11 @@ def _ragged(T, state, cu_seqlens, slots, fresh, max_len):
                          _addr(slots), _addr(fresh))
 
 
+def _same_steps(a, b):
+    """Tensors of one shape whose elements lie alike: the stride of a dim of size 1 is never stepped."""
+    return a.stride() == b.stride() or all(n == 1 or x == y for n, x, y in zip(a.shape, a.stride(), b.stride()))
+
+
 def _gdn_ragged_args(q, k, v, g, beta, state, cu_seqlens, slots, fresh, max_len, o):
     if q.dim() != 3 or v.dim() != 3:
         raise ValueError("q, k must be [T, Hk, Dk] and v [T, Hv, Dv]")
@@ -647,14 +652,14 @@ def _gdn_ragged_args(q, k, v, g, beta, state, cu_seqlens, slots, fresh, max_len,
         raise TypeError(f"unsupported I/O dtype {q.dtype}")
     (T, Hk, Dk), (Tv, Hv, Dv) = q.shape, v.shape
     qs, vs, gs, ss = q.stride(), v.stride(), g.stride(), state.stride()
-    if k.shape != q.shape or k.stride() != qs or k.dtype != q.dtype:
+    if k.shape != q.shape or not _same_steps(k, q) or k.dtype != q.dtype:
         raise ValueError("q and k must share shape, strides and dtype")
     if Tv != T or v.dtype != q.dtype:
         raise ValueError("v must have the tokens and the dtype of q")
     if qs[2] != 1 or vs[2] != 1:
         raise ValueError("the channel dim must be contiguous")
     for name, t in (("g", g), ("beta", beta)):
-        if t.shape != (T, Hv) or t.dtype != torch.float32 or t.stride() != gs:
+        if t.shape != (T, Hv) or t.dtype != torch.float32 or not _same_steps(t, g):
             raise ValueError(f"{name} must be float32 [{T}, {Hv}], with the strides of g")
     if state.dim() != 4 or state.shape[1:] != (Hv, Dk, Dv) or state.dtype != torch.float32 \
             or (state.numel() and ss[1:] != (Dk * Dv, Dv, 1) and not state[0].is_contiguous()):

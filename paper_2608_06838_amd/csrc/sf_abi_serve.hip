@@ -83,8 +83,9 @@ Range pool_range(const char *name, const float *p, int32_t n_slots, int64_t per,
     return span(p, n_slots > 0 ? 4 * ((n_slots - 1) * ss + per) : 0, name);
 }
 
-sf_status grid_fits(double workgroups) {
-    return workgroups < 2147483647.0 ? SF_OK : fail(SF_E_UNSUPPORTED, "batch too large for one call");
+// a launch counts its threads in 32 bits
+sf_status grid_fits(double threads) {
+    return threads < 4294967296.0 ? SF_OK : fail(SF_E_UNSUPPORTED, "batch too large for one call");
 }
 sf_status launched(hipError_t e) { return e == hipSuccess ? SF_OK : hip_fail(e, "kernel launch"); }
 
@@ -317,8 +318,9 @@ sf_status sf_gdn_ragged_fwd(const sf_gdn_ragged_shape *shape, const sf_ragged *b
         a.o = o;
         a.ws = (char *)ws;
         a.plan = need ? (int32_t *)(a.ws + sf::gdn_plan_at(a)) : nullptr;
-        const double tok = (double)sf::gdn_token_waves(a);  // workgroups hold four
-        TRY(grid_fits(std::max(tok + sf::gdn_walk_groups(a), (double)a.n_chunks * s.Hk + 1)));
+        // waves of 64, a workgroup's four at most idle
+        const double tok = 64.0 * (double)(sf::gdn_token_waves(a) + 4), walk = 256.0 * (double)sf::gdn_walk_groups(a);
+        TRY(grid_fits(a.longer ? std::max(tok + walk, 256.0 * ((double)a.n_chunks * s.Hk + 1)) : tok));
         sf_timing *const tm = timing_of(tuning);
         hipEvent_t e0, e1;
         if (!a.longer) {
@@ -375,7 +377,7 @@ sf_status sf_conv_ragged_fwd(const sf_conv_ragged_shape *shape, const sf_ragged 
         a.sx_t = s.sx_t;
         a.sy_t = s.sy_t;
         a.ss = s.ss;
-        TRY(grid_fits((double)a.n_runs * ((s.C / 8 + 63) / 64)));
+        TRY(grid_fits((double)a.n_runs * ((s.C / 8 + 255) / 256 * 256)));
         hipEvent_t e0, e1;
         take_pair(timing_of(tuning), SF_K_CONV_RAGGED, e0, e1);
         return launched(sf::launch_conv_ragged(a, (hipStream_t)stream, e0, e1));

@@ -1,6 +1,7 @@
 // Host-side checks, under sanitizers, of how the ragged delta rule numbers its chunk
 // systems: room for every chunk of every long sequence, none shared, a workgroup finds its
-// sequence by the last first number at most its own, and short sequences cost no workspace.
+// sequence by the last first number at most its own, and short sequences cost no workspace;
+// and of the largest launches.
 #include <algorithm>
 #include <cstdint>
 #include <cstdio>
@@ -67,6 +68,21 @@ int main() {
                 if (sf::gdn_first_system(a, cu[i], i) <= id) found = i;
             EXPECT(owner[id] == -1 || owner[id] == found);
         }
+    }
+    // a launch holds fewer than 2^32 threads: more are refused before anything is launched
+    for (int over = 0; over < 2; ++over) {
+        sf::ServeRecord rec;
+        sf::serve_record = over ? nullptr : &rec;
+        auto at = [](uint64_t i) { return (void *)(uintptr_t)(i << 48); };
+        sf_conv_ragged_shape c = {4096, 1, SF_BF16, SF_ACT_NONE, 0, 0, 4096, 0};
+        const int N = over ? 1 << 23 : (1 << 23) - 8192;
+        sf_ragged b = {N, 1, 64, 1, (const int32_t *)at(1), (const int32_t *)at(2), nullptr};
+        EXPECT(sf_conv_ragged_fwd(&c, &b, at(3), (const float *)at(4), nullptr, at(5), nullptr, nullptr) ==
+               (over ? SF_E_UNSUPPORTED : SF_OK));
+        sf_gdn_ragged_shape s = {16, 16, 128, 128, SF_BF16, 0, 0, 0, 0, 0, 16 * 128, 128, 0, 0, 16 * 128 * 128};
+        b.N = over ? 1 << 20 : (1 << 20) - 1024;
+        EXPECT(sf_gdn_ragged_fwd(&s, &b, at(3), at(4), at(6), (const float *)at(7), (const float *)at(8), (float *)at(9),
+                                 at(5), nullptr, 0, nullptr, nullptr) == (over ? SF_E_UNSUPPORTED : SF_OK));
     }
     EXPECT(with_few > 500 && with_few < 3500);
     if (failures) return 1;

@@ -848,6 +848,8 @@ def qk_norm_bwd(q, k, dyq, dyk, *, norm="l2", q_weight=None, k_weight=None, eps=
     outputs (the last three None without weights)."""
     dq, dk, dwq, dwk, ws = (None,) * 5 if out is None else out
     weights = q_weight is not None
+    if not weights and (dwq is not None or dwk is not None):
+        raise ValueError("dwq and dwk are gradients of weights, and there are none")
     dev, sh, pos = _qk_args(q, k, norm, q_weight, k_weight, eps, q_scale, inv_freq, pos, pos0, interleaved, dyq, dyk,
                             dq, dk)
     for name, t in (("dwq", dwq), ("dwk", dwk)) if out is not None else ():

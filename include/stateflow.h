@@ -480,6 +480,7 @@ sf_status sf_gdn_chain_bwd(const sf_shape *shape, int32_t n_seg, const int64_t *
  *            a zero state, whatever its slot holds.
  * A sequence of no tokens leaves its slot as it was.  Slots that no sequence
  * names are not touched.
+ * A launch has fewer than 2^32 threads; a larger batch is refused (SF_E_UNSUPPORTED).
  */
 typedef struct sf_ragged {
     int32_t N, n_slots;
@@ -507,7 +508,10 @@ typedef struct sf_ragged {
  * Inputs may be broadcast (stride 0).  No allocation, no synchronisation.
  * Short sequences, and all with SF_F32, run token by token; with SF_BF16 and a max_len
  * above 12 (24 where the launch has more than a wave a CU), longer ones run in chunks of
- * 64 tokens, which takes the workspace (contents on entry ignored, 16-byte aligned).
+ * 64 tokens, which takes the workspace (contents on entry ignored, 16-byte aligned): 31 KB
+ * a value head for each of T / 64 + N chunks, or of T / 13 (T / 25) where that is less.
+ * Either way states come out as from fp32 arithmetic, and outputs of SF_BF16 are that
+ * rounded once.
  * g = -inf forgets the state.  A NaN or infinity elsewhere spoils its own sequence, from
  * its token on or from the start of that token's chunk, and no other.
  */
@@ -566,6 +570,9 @@ sf_status sf_conv_ragged_fwd(const sf_conv_ragged_shape *shape, const sf_ragged 
  * reproducible); the norm's factor is computed again from q and k.
  * Supported: D a multiple of 16 up to 256, R a multiple of 16 up to D, 16-byte
  * aligned pointers and strides (inputs may be broadcast), fewer than 2^31 tokens.
+ * Outputs may lie between other tensors (slices of one buffer, along any dims) with
+ * which they share no element.  Sums of squares are held in fp32: a row whose sum leaves
+ * its range (entries beyond about 10^18) counts as infinitely long, and its r is 0.
  */
 typedef enum { SF_NORM_NONE = 0, SF_NORM_L2 = 1, SF_NORM_RMS = 2 } sf_norm;
 

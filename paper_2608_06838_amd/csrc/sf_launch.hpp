@@ -158,8 +158,8 @@ struct GdnRaggedArgs {
 // waves of the token-by-token kernel: one for each sequence, value head and tile of 4 cl
 // columns.  TOK_CL column lanes take whole 128-byte lines of the state; half of them make
 // a token cheaper for a wave, and pay while there is a SIMD for each (16 tokens of 20
-// heads of 128, us with 8 / 4 lanes: one sequence 17.8 / 14.4, 8 sequences 19.6 / 21.5,
-// 64 67 / 85): launches of at most TOK_FEW full waves a CU.
+// heads of 128, us with 8 / 4 lanes: one sequence 17.8 / 15.4, 8 sequences 19.7 / 22.1,
+// 64 71 / 96): launches of at most TOK_FEW full waves a CU.
 constexpr int TOK_CL = 8, TOK_FEW = 2;
 inline int64_t gdn_token_waves(const GdnRaggedArgs &a, int cl = TOK_CL) { return (int64_t)a.r.N * a.Hv * (a.Dv / (4 * cl)); }
 // A chunk's triangular system: T = (I + A)^-1 as operand fragments in three bf16 planes
@@ -168,9 +168,9 @@ inline int64_t gdn_token_waves(const GdnRaggedArgs &a, int cl = TOK_CL) { return
 constexpr int RAG_FRAGS = 6, RAG_TP = 3, RAG_R = RAG_TP * RAG_FRAGS * 1024, RAG_GATES = RAG_R + 12 * 1024, RAG_SYS = RAG_GATES + 1024;
 // Sequences up to so many tokens are taken token by token: a chunk costs the same
 // whatever its tokens, a token what the CUs' other waves leave it (20 heads of 128, us in
-// chunks / token by token: one sequence of 8 tokens 12.8 / 8.9, of 12 12.9 / 11.7, of 16
-// 12.9 / 14.4; 64 sequences of 16 tokens 86 / 67, of 24 91 / 89, of 32 91 / 114; 256 of 24
-// with 40 heads 674 / 637, of 32 696 / 839).
+// chunks / token by token: one sequence of 8 tokens 13.4 / 9.2, of 12 13.3 / 12.0, of 16
+// 13.4 / 15.1; 64 sequences of 16 tokens 101 / 72, of 24 99 / 98, of 32 99 / 122; 256 of 24
+// with 40 heads 697 / 632, of 32 720 / 856).
 constexpr int RAG_LONG = 24, RAG_LONG_FEW = 12;
 static_assert(RAG_LONG < 32 && RAG_LONG_FEW < 32, "n / (longer + 1) >= ceil(n / 64) from longer + 1 tokens on");
 inline int gdn_long(const GdnRaggedArgs &a) { return gdn_token_waves(a) <= a.n_cu ? RAG_LONG_FEW : RAG_LONG; }
@@ -218,7 +218,7 @@ struct ConvRaggedArgs {
     int64_t sx_t, sy_t, ss;
 };
 // Tokens of a run: 32 keep the halo rows, read twice, under a tenth (8259 tokens of
-// 15360 channels: runs of 8 143 us, 16 129, 32 127, 64 134), 8 (one load group) where
+// 15360 channels: runs of 8 118 us, 16 99, 32 101, 64 113), 8 (one load group) where
 // longer ones would leave the chip short of threads (CONV_FILL).
 inline int conv_ragged_run(int64_t T, int64_t N, int64_t C, int n_cu) {
     int run = 32;

@@ -18,8 +18,8 @@
 // in the same one (interleaved); where it is in another, the raw 16-bit values
 // cross over, half the traffic of finished ones, and cos and sin come with the
 // weights of both channels multiplied in.  Calls with few tokens share a token's
-// heads between waves (qk_plan).  32K tokens of 80 heads of 128, bf16: 251 us forward,
-// 396 backward, 5.3 and 5.1 TB/s where a copy reaches 4.9.
+// heads between waves (qk_plan).  32K tokens of 80 heads of 128, bf16: 249 us forward,
+// 371 backward, 5.4 TB/s where a copy reaches 4.9.
 #include "sf_device.hpp"
 #include "sf_launch.hpp"
 
@@ -34,8 +34,8 @@ constexpr int QK_NT = 64 * QK_W;
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 
 // 8 consecutive channels as they lie in memory.  Loads and stores are non-temporal:
-// nothing is read twice (32K tokens of 80 heads of 128, bf16: forward 267 us with plain
-// ones, 259 with stores alone, 256 with both; backward 416, 413, 399).
+// nothing is read twice (32K tokens of 80 heads of 128, bf16: forward 262 us with plain
+// ones, 254 with stores alone, 249 with both; backward 391, 390, 371).
 template <typename T>
 struct Oct {
     static constexpr int NV = 8 * (int)sizeof(T) / 16;

@@ -53,7 +53,7 @@ __device__ __forceinline__ int64_t first_run(const Seq &s, int run, int i) { ret
 // so a token costs one reduction over the row groups, of nine sums.  Several tokens' decay
 // is kept as one factor beside the state (a quarter of a token's work would go into
 // applying it), applied when it leaves [1e-9, 16] and at the end.  The state goes past
-// the caches (256 sequences of 40 heads of 128 x 128: 245 us, 5.5 TB/s; 272 through them).
+// the caches (256 sequences of 40 heads of 128 x 128: 235 us, 5.7 TB/s; 258 through them).
 constexpr int TOK_NT = 256;
 
 // sum over the row groups (lanes that differ in the bits from CL up), in every lane

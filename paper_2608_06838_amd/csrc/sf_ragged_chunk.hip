@@ -148,8 +148,8 @@ __device__ __forceinline__ constexpr int tri_tile16(int tt, int c) { return 2 * 
 // steers the schedule alone).  A sequence with more chunks than a CU's share of all
 // chunk steps is what the launch waits for: it is walked in single column tiles, whose
 // step is shorter, as long as each has a CU of its own; the others in pairs of tiles,
-// which share what a chunk loads.  (Chunk steps, us: alone on a CU 2.2 single, 3.4 in
-// pairs; with the CUs full 1.9 a single tile, 2.8 a pair.)  One workgroup.
+// which share what a chunk loads.  (Chunk steps, us: alone on a CU 2.2 single, 3.1 in
+// pairs; with the CUs full 2.1 a single tile, 3.1 a pair.)  One workgroup.
 constexpr int PLAN_B = 128;
 __device__ __forceinline__ int plan_bucket(int64_t n) {
     const unsigned c = (unsigned)((n + 63) / 64);  // 1 .. 2^25
@@ -722,8 +722,8 @@ __global__ void __launch_bounds__(256, 2) k_rag_walk(GdnRaggedArgs a, int groups
     }
     const int count = __builtin_amdgcn_readfirstlane(a.plan[0]), single = __builtin_amdgcn_readfirstlane(a.plan[1]);
     // lines are fetched two chunks ahead while all items run at once (16384 tokens of 40
-    // heads: 787 us against 864; three prompts of 4096 of 20 heads 213 against 228; but 32 of
-    // 1024, five items to a place: 486 against 478)
+    // heads: 992 us against 1009; but 32 prompts of 1024 of 20 heads, five items to a place:
+    // 584 against 577)
     const int64_t one = gdn_walk_items(a, single, 1), pairs = gdn_walk_items(a, count - single, 2);
     const bool reach = one + pairs <= 2 * (int64_t)a.n_cu;
     rag_walk_items<DK, 1>(a, mem, 0, single, 0, groups, reach);

@@ -227,15 +227,16 @@ bool side_by_side(const Heads &a, const Heads &b, const sf_qk_shape &s, size_t e
     if ((uintptr_t)a.p > (uintptr_t)b.p) return side_by_side(b, a, s, e);
     const uint64_t d = (uintptr_t)b.p - (uintptr_t)a.p;
     const int64_t E = (int64_t)e;
-    const Dim da[3] = {{s.B, a.t.b * E}, {s.L, a.t.l * E}, {a.H, a.t.h * E}};
-    const Dim db[3] = {{s.B, b.t.b * E}, {s.L, b.t.l * E}, {b.H, b.t.h * E}};
+    auto dim = [&](int64_t size, int64_t stride) { return Dim{size, size > 1 ? stride * E : 0}; };  // of one: never stepped
+    const Dim da[3] = {dim(s.B, a.t.b), dim(s.L, a.t.l), dim(a.H, a.t.h)};
+    const Dim db[3] = {dim(s.B, b.t.b), dim(s.L, b.t.l), dim(b.H, b.t.h)};
     for (int outer = 1; outer < 8; ++outer) {
         std::vector<Dim> cells;
         uint64_t ea = (uint64_t)(s.D * E), eb = ea;
         bool alike = true;
         for (int i = 0; i < 3; ++i) {
             if (outer >> i & 1) {
-                alike = alike && da[i].size == db[i].size && (da[i].size == 1 || da[i].stride == db[i].stride);
+                alike = alike && da[i].size == db[i].size && da[i].stride == db[i].stride;
                 cells.push_back(da[i]);
             } else {
                 ea += (uint64_t)((da[i].size - 1) * da[i].stride);

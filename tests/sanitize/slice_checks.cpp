@@ -67,6 +67,12 @@ int main() {
         EXPECT(fwd(s, 0, L * Hk * D) == SF_OK);
         EXPECT(fwd(s, 0, L * Hk * D - 8) == SF_E_ALIAS);
     }
+    {  // a single token's stride may be anything
+        sf_qk_shape s = shape(B, 1, Hq, Hk, D);
+        s.yq = {(Hq + Hk) * D, INT64_MAX - 7, D}, s.yk = {(Hq + Hk) * D, 8, D};
+        EXPECT(fwd(s, 0, Hq * D) == SF_OK);
+        EXPECT(fwd(s, 0, Hq * D - 8) == SF_E_ALIAS);
+    }
     // whatever is accepted shares no element
     std::mt19937 rng(1);
     auto pick = [&](int lo, int hi) { return (int64_t)std::uniform_int_distribution<int>(lo, hi)(rng); };

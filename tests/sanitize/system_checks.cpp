@@ -28,8 +28,8 @@ static size_t workspace(int N, int64_t T, int64_t max_len, int Hv) {
 }
 
 int main() {
-    // 1024 single tokens beside a prompt of 2048, 40 heads: systems of the tokens over 25, not of 1024 sequences
-    EXPECT(workspace(1025, 3072, 2048, 40) <= (size_t)(3072 / 25) * 40 * sf::RAG_SYS + 4 * 1027);
+    // 1000 single tokens beside a prompt of 2000, 40 heads: systems of the tokens over 25, not of 1001 sequences
+    EXPECT(workspace(1001, 3000, 2000, 40) <= (size_t)(3000 / 25) * 40 * sf::RAG_SYS + 4 * 1003);
     // prompts alone: a system for every 64 tokens and one a sequence
     EXPECT(workspace(8, 8192, 2000, 40) == (size_t)(8192 / 64 + 8) * 40 * sf::RAG_SYS + 4 * 10);
     // no sequence can be long
